@@ -75,7 +75,7 @@ typedef enum { FFF_F32 = 0, FFF_BF16 = 1 } fff_dtype;
 
 /* The paper does not name the leaf activation; ReLU and exact GELU
  * v * Phi(v) = 0.5 v (1 + erf(v / sqrt 2)) are offered. */
-typedef enum { FFF_ACT_RELU = 0, FFF_ACT_GELU = 1 } fff_act;
+typedef enum { FFF_ACT_RELU = 0, FFF_ACT_GELU = 1, FFF_ACT_NONE = 2 /* fff_mx4_product only */ } fff_act;
 
 #define FFF_MAX_DEPTH 24
 
@@ -202,6 +202,114 @@ int fff_moe_top1_forward(const void* x, const void* gate_w, const void* gate_b,
                          const void* leaf_b2, int log2_experts, int leaf_width, int act,
                          void* out, int32_t* expert_idx, void* stream,
                          int64_t T, int64_t D, int64_t O, int dtype);
+
+/*
+ * fff_moe_route: the choice of k experts per token from gating logits, with what a mixture is trained on
+ * beside its outputs.  Per token: the k largest logits in descending order (the lowest index first among equal
+ * ones; a NaN logit counts as -infinity, and -infinity is never chosen: a token with fewer than k others gets
+ * index -1 and weight 0 in the slots behind them).  p = softmax of the token's logits (logits of +infinity
+ * share all of it); the weights are p at the chosen experts, divided by their sum when `normalise`.
+ *   logits      [T, n_experts], dtype FFF_F32 or FFF_BF16; n_experts 1..4096
+ *   token_mask  [T] bytes or NULL; a token whose byte is 0 takes no part: -1, weight 0, not counted.  Nor does
+ *               a token whose logits are all -infinity or NaN.  n = the tokens that take part.
+ *   k           1..min(n_experts, 32)
+ *   expert_idx  [T, k] int32; weight [T, k] fp32
+ *   count       [n_experts + 1] int32 or NULL: tokens per expert, then n
+ *   prob_mean   [n_experts] fp32 or NULL: mean of p over the n tokens
+ *   loss        [2] fp32 or NULL: the balance loss n_experts * sum_e (count[e] / (n k)) * prob_mean[e], which is 1
+ *               for an even load, and the z loss, the mean over the n tokens of (log sum exp of the logits)^2;
+ *               n = 0: zeros
+ *   scratch     device memory, 256-byte aligned, at least fff_route_scratch_bytes of the same sizes, of one
+ *               call from its launches until they have run; needs no initial value.  Only read where one of
+ *               count, prob_mean and loss is given (they are then written for T = 0 too); else it may be NULL.
+ * Sums are fp32 in an order that depends on the sizes alone.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T,
+ * n_experts, k), FFF_ERR_SHAPE (T * n_experts beyond 2^40), FFF_ERR_DTYPE, FFF_ERR_WORKSPACE, FFF_ERR_ALIAS (an output overlaps logits or
+ * scratch), FFF_ERR_DEVICE.
+ */
+int fff_moe_route(const void* logits, const uint8_t* token_mask, int64_t n_experts, int k, int normalise,
+                  int32_t* expert_idx, float* weight, int32_t* count, float* prob_mean, float* loss,
+                  void* stream, int64_t T, int dtype, void* scratch, size_t scratch_bytes);
+size_t fff_route_scratch_bytes(int64_t T, int64_t n_experts);
+
+/*
+ * fff_moe_route_backward: the gradient of fff_moe_route's weights and losses to the logits (the choice itself
+ * and the counts are constants).  logits, token_mask, k, normalise as in the call before; expert_idx and
+ * count are what it wrote.
+ *   dweight  [T, k] fp32 or NULL (zeros): gradient of the weights; slots whose index is -1 (or no expert's) are not read
+ *   dloss    [2] fp32 on the device, or NULL (zeros): gradients of the balance loss and the z loss; needs count
+ *   dlogits  [T, n_experts], the dtype of logits: every row written, zeros for a token that takes no part
+ * A logit of +infinity has a z loss of infinity, and its gradient is infinite where p > 0.  Needs no scratch.
+ * Errors: as for fff_moe_route.
+ */
+int fff_moe_route_backward(const void* logits, const uint8_t* token_mask, int64_t n_experts, int k,
+                           int normalise, const int32_t* expert_idx, const int32_t* count,
+                           const float* dweight, const float* dloss, void* dlogits, void* stream, int64_t T,
+                           int dtype);
+
+/*
+ * Four-bit matrices.  A row of n elements is ceil(n / 32) blocks of 32; a block is a scale byte s, which stands
+ * for 2^(s - 127) (255: the whole block is NaN), and 32 codes of 4 bits -- sign, two exponent bits, one mantissa
+ * bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives -- two to a byte, the earlier element in the low four
+ * bits.  Codes are [rows, 16 ceil(n / 32)] bytes (16-byte aligned), scales [rows, ceil(n / 32)] bytes;
+ * the codes behind a row's end are zeros.  (The layout of the OCP microscaling format MXFP4.)
+ *
+ * fff_mx4_quantize: per block s = floor(log2(largest magnitude)) - 2 + 127, at least 0; each element is divided by the
+ * scale, rounded to the nearest value above (ties to the even mantissa) and limited to +-6.  A block that holds
+ * an infinity or NaN becomes scale 255 and zero codes; a block of zeros scale 0.
+ *   src        [batch, rows, cols], dtype FFF_F32 or FFF_BF16
+ *   transpose  0: codes and scales of the rows, [batch, rows, ...]; else of the columns, [batch, cols, ...] with blocks
+ *              along `rows` (leaf_w2 [leaves, leaf_width, O] for fff_leaf_forward_mx4)
+ * Errors: FFF_ERR_NULL, FFF_ERR_SHAPE (rows or cols < 1, or more than 2^40 elements), FFF_ERR_RANGE (batch < 0),
+ * FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (codes misaligned), FFF_ERR_ALIAS (codes or scales overlap src or each other), FFF_ERR_DEVICE.
+ * batch == 0 is FFF_OK.
+ *
+ * fff_mx4_dequantize: the values, [rows, cols] of `dtype` (exact in both).
+ */
+int fff_mx4_quantize(const void* src, uint8_t* codes, uint8_t* scales, int transpose, void* stream,
+                     int64_t batch, int64_t rows, int64_t cols, int dtype);
+int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, void* stream, int64_t rows,
+                       int64_t cols, int dtype);
+
+/*
+ * fff_mx4_product: out = act(A W^T + bias) with W in four bits; fp32 accumulation, one rounding at the end.
+ *   a         [T, K]: bf16 when a_scales is NULL, else codes with scales a_scales (fff_mx4_quantize)
+ *   w, w_scales   codes and scales of [N, K]
+ *   bias      [N] of `dtype`, or NULL
+ *   act       FFF_ACT_NONE, FFF_ACT_RELU or FFF_ACT_GELU
+ *   out       [T, N] of `dtype` (FFF_F32 only with a_scales: bf16 rows give bf16 results, else FFF_ERR_UNSUPPORTED)
+ *   scratch   device memory, 256-byte aligned, of one call until its launches have run, at least
+ *             fff_mx4_product_scratch_bytes: a copy of bf16 rows that are not whole aligned pieces of 16 bytes (K not a
+ *             multiple of 8, or a misaligned); never read otherwise, and may be NULL then
+ * K <= 2^24, N <= 2^24.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T), FFF_ERR_SHAPE, FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (act, or misaligned codes),
+ * FFF_ERR_ALIAS (out or scratch overlaps an input or each other), FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.
+ */
+int fff_mx4_product(const void* a, const uint8_t* a_scales, const uint8_t* w, const uint8_t* w_scales,
+                    const void* bias, int act, void* out, void* stream, int64_t T, int64_t K, int64_t N,
+                    int dtype, void* scratch, size_t scratch_bytes);
+size_t fff_mx4_product_scratch_bytes(int64_t T, int64_t K);
+
+/*
+ * fff_leaf_forward_mx4: fff_leaf_forward with the leaves' matrices in four bits, any number of leaves, and k of them
+ * per token: out[t] = sum over i < k of weight[t][i] * leaf(leaf_idx[t][i], x[t]).  What fff_moe_route chose, or, with k = 1
+ * and no weights, what fff_descend reached.  Indices outside [0, n_leaves) are no leaf and add nothing (a token
+ * with none: zeros); the same leaf twice counts twice.
+ *   x [T, D] bf16; leaf_w1, leaf_s1: codes and scales of [n_leaves, leaf_width, D]; leaf_b1 [n_leaves, leaf_width];
+ *   leaf_w2, leaf_s2: codes and scales of [n_leaves, O, leaf_width] (of leaf_w2 [n_leaves, leaf_width, O]:
+ *   fff_mx4_quantize with transpose); leaf_b2 [n_leaves, O]; biases bf16
+ *   leaf_idx [T, k] int32, weight [T, k] fp32 or NULL (ones); k 1..32; n_leaves 1..65536; leaf_width 1..65536
+ *   act FFF_ACT_RELU or FFF_ACT_GELU; out [T, O] bf16, must not overlap x; dtype must be FFF_BF16 (else FFF_ERR_UNSUPPORTED)
+ *   scratch  device memory, 256-byte aligned, of one call until its launches have run, at least
+ *            fff_leaf_mx4_scratch_bytes of the same sizes; needs no initial value
+ * Hidden activations are rounded to bf16 (the operand type of the matrix cores), sums are fp32.  Results do not depend on the
+ * order in which tokens are grouped.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T, k, n_leaves, leaf_width), FFF_ERR_SHAPE, FFF_ERR_DTYPE,
+ * FFF_ERR_UNSUPPORTED, FFF_ERR_ALIAS, FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.
+ */
+int fff_leaf_forward_mx4(const void* x, const uint8_t* leaf_w1, const uint8_t* leaf_s1, const void* leaf_b1,
+                         const uint8_t* leaf_w2, const uint8_t* leaf_s2, const void* leaf_b2,
+                         const int32_t* leaf_idx, const float* weight, int64_t n_leaves, int k, int leaf_width,
+                         int act, void* out, void* stream, int64_t T, int64_t D, int64_t O, int dtype,
+                         void* scratch, size_t scratch_bytes);
+size_t fff_leaf_mx4_scratch_bytes(int64_t T, int64_t D, int64_t O, int64_t n_leaves, int k, int leaf_width);
 
 /*
  * fff_forward_soft: Forward_T of Algorithm 1, the soft pass used in training and

@@ -19,10 +19,12 @@ from . import build as _build
 
 ACT_RELU = 0
 ACT_GELU = 1
+ACT_NONE = 2    # fff_mx4_product only
 DTYPE_F32 = 0
 DTYPE_BF16 = 1
 ERR_SHAPE = 2
 ERR_DTYPE = 3
+ERR_WORKSPACE = 6
 MAX_DEPTH = 24
 
 
@@ -67,6 +69,18 @@ def lib() -> ctypes.CDLL:
         L.fff_bucket.argtypes = [vp, i64, i32, vp, vp, vp, vp]
         L.fff_leaf_forward.argtypes = [vp] * 6 + [i32, i32, i32, vp, vp, i64, i64, i64, i32]
         L.fff_moe_top1_forward.argtypes = [vp] * 7 + [i32, i32, i32, vp, vp, vp, i64, i64, i64, i32]
+        L.fff_moe_route.argtypes = [vp, vp, i64, i32, i32] + [vp] * 6 + [i64, i32, vp, ctypes.c_size_t]
+        L.fff_route_scratch_bytes.argtypes = [i64, i64]
+        L.fff_route_scratch_bytes.restype = ctypes.c_size_t
+        L.fff_moe_route_backward.argtypes = [vp, vp, i64, i32, i32] + [vp] * 6 + [i64, i32]
+        L.fff_mx4_quantize.argtypes = [vp, vp, vp, i32, vp, i64, i64, i64, i32]
+        L.fff_mx4_dequantize.argtypes = [vp, vp, vp, vp, i64, i64, i32]
+        L.fff_mx4_product.argtypes = [vp] * 5 + [i32, vp, vp, i64, i64, i64, i32, vp, ctypes.c_size_t]
+        L.fff_mx4_product_scratch_bytes.argtypes = [i64, i64]
+        L.fff_mx4_product_scratch_bytes.restype = ctypes.c_size_t
+        L.fff_leaf_forward_mx4.argtypes = [vp] * 9 + [i64, i32, i32, i32, vp, vp, i64, i64, i64, i32, vp, ctypes.c_size_t]
+        L.fff_leaf_mx4_scratch_bytes.argtypes = [i64, i64, i64, i64, i32, i32]
+        L.fff_leaf_mx4_scratch_bytes.restype = ctypes.c_size_t
         L.fff_forward_soft.argtypes = [vp] * 7 + [i32, i32, i32, vp, vp, vp, vp, i64, i64, i64, i32]
         L.fff_forward_block.argtypes = ([vp] * 3 + [ctypes.c_float] + [vp] * 8 + [i32] * 5 + [vp, vp, vp] +
                                         [i64, i64, i64, i32])
@@ -303,6 +317,167 @@ def fff_moe_top1_forward(x, gate_w, gate_b, leaf_w1, leaf_b1, leaf_w2, leaf_b2, 
                                       _ptr(leaf_w2), _ptr(leaf_b2), log2_experts, leaf_width, act, _ptr(out),
                                       _ptr(expert_idx), _stream_handle(stream), T, D, O, _dtype_code(x)),
            where)
+
+
+def _size(where: str, name: str, t, dims) -> tuple:
+    """The sizes of a tensor that the others' are derived from."""
+    if t is None or t.dim() not in dims:
+        raise FffError(ERR_SHAPE, where, "%s must have %s dimensions" % (name, " or ".join(str(d) for d in dims)))
+    return tuple(int(n) for n in t.shape)
+
+
+def _check_here(*tensors) -> None:
+    """Dense, and on the device that the call's kernels and scratch are on: the current one."""
+    import torch
+    _check_dense(*tensors)
+    for t in tensors:
+        if t is not None and t.get_device() != torch.cuda.current_device():
+            raise ValueError("FFF tensors must live on the current device")
+
+
+def _scratch(where: str, nbytes: int, stream):
+    buf = _torch_scratch(nbytes, stream)
+    if buf is None:
+        raise FffError(ERR_WORKSPACE, where, "no scratch of %d bytes to be had from torch's allocator (out of memory, or a capture that "
+                       "is not torch's)" % nbytes)
+    return buf
+
+
+def fff_moe_route(logits, k, expert_idx, weight, count=None, prob_mean=None, loss=None, token_mask=None, normalise=True, stream=None) -> None:
+    """The k experts of every token of logits [T, E] -> expert_idx [T, k] int32, weight [T, k] float32; with any of count [E + 1]
+    int32, prob_mean [E] and loss [2] float32 also what the tokens have in common: tokens per expert (and in all), mean probabilities,
+    the balance loss and the z loss.  token_mask [T] uint8 or bool: tokens that take part."""
+    import torch
+    where = "fff_moe_route"
+    T, E = _size(where, "logits", logits, (2,))
+    _expect(where, "expert_idx", expert_idx, (T, k), torch.int32)
+    _expect(where, "weight", weight, (T, k), torch.float32)
+    _expect(where, "count", count, (E + 1,), torch.int32)
+    _expect(where, "prob_mean", prob_mean, (E,), torch.float32)
+    _expect(where, "loss", loss, (2,), torch.float32)
+    _expect(where, "token_mask", token_mask, (T,), torch.bool if token_mask is not None and token_mask.dtype == torch.bool else torch.uint8)
+    _check_here(logits, expert_idx, weight, count, prob_mean, loss, token_mask)
+    need, scratch = 0, None
+    if count is not None or prob_mean is not None or loss is not None:
+        need = fff_route_scratch_bytes(T, E)
+        scratch = _scratch(where, need, stream) if need else None
+    _check(lib().fff_moe_route(_ptr(logits), _ptr(token_mask), E, k, int(bool(normalise)), _ptr(expert_idx), _ptr(weight), _ptr(count),
+                               _ptr(prob_mean), _ptr(loss), _stream_handle(stream), T, _dtype_code(logits), _ptr(scratch), need), where)
+
+
+def fff_route_scratch_bytes(T: int, n_experts: int) -> int:
+    return int(lib().fff_route_scratch_bytes(T, n_experts))
+
+
+def fff_moe_route_backward(logits, expert_idx, count, dlogits, dweight=None, dloss=None, token_mask=None, normalise=True, stream=None) -> None:
+    """dlogits [T, E] from the gradients of fff_moe_route's weights (dweight [T, k]) and losses (dloss [2], on the GPU), float32 both; expert_idx
+    and count as that call wrote them."""
+    import torch
+    where = "fff_moe_route_backward"
+    T, E = _size(where, "logits", logits, (2,))
+    k = _size(where, "expert_idx", expert_idx, (2,))[1]
+    _expect(where, "expert_idx", expert_idx, (T, k), torch.int32)
+    _expect(where, "count", count, (E + 1,), torch.int32)
+    _expect(where, "dlogits", dlogits, (T, E), logits.dtype)
+    _expect(where, "dweight", dweight, (T, k), torch.float32)
+    _expect(where, "dloss", dloss, (2,), torch.float32)
+    _expect(where, "token_mask", token_mask, (T,), torch.bool if token_mask is not None and token_mask.dtype == torch.bool else torch.uint8)
+    _check_here(logits, expert_idx, count, dlogits, dweight, dloss, token_mask)
+    _check(lib().fff_moe_route_backward(_ptr(logits), _ptr(token_mask), E, k, int(bool(normalise)), _ptr(expert_idx), _ptr(count),
+                                        _ptr(dweight), _ptr(dloss), _ptr(dlogits), _stream_handle(stream), T, _dtype_code(logits)), where)
+
+
+def _mx4_blocks(n: int) -> int:
+    return (n + 31) // 32
+
+
+def fff_mx4_quantize(src, codes, scales, transpose=False, stream=None) -> None:
+    """src [rows, cols] or [batch, rows, cols] -> four-bit codes [..., rows, 16 ceil(cols / 32)] and scales [..., rows, ceil(cols / 32)],
+    uint8 both; with transpose those of the columns, [..., cols, 16 ceil(rows / 32)] and [..., cols, ceil(rows / 32)]."""
+    import torch
+    where = "fff_mx4_quantize"
+    shape = _size(where, "src", src, (2, 3))
+    rows, cols = shape[-2:]
+    r, c = (cols, rows) if transpose else (rows, cols)
+    _expect(where, "codes", codes, shape[:-2] + (r, 16 * _mx4_blocks(c)), torch.uint8)
+    _expect(where, "scales", scales, shape[:-2] + (r, _mx4_blocks(c)), torch.uint8)
+    _check_here(src, codes, scales)
+    _check(lib().fff_mx4_quantize(_ptr(src), _ptr(codes), _ptr(scales), int(bool(transpose)), _stream_handle(stream),
+                                  shape[0] if len(shape) == 3 else 1, rows, cols, _dtype_code(src)), where)
+
+
+def fff_mx4_dequantize(codes, scales, out, stream=None) -> None:
+    """out [..., rows, cols] <- the values of codes [..., rows, 16 ceil(cols / 32)] and scales [..., rows, ceil(cols / 32)]."""
+    import torch
+    where = "fff_mx4_dequantize"
+    shape = _size(where, "out", out, (2, 3))
+    blocks = _mx4_blocks(shape[-1])
+    _expect(where, "codes", codes, shape[:-1] + (16 * blocks,), torch.uint8)
+    _expect(where, "scales", scales, shape[:-1] + (blocks,), torch.uint8)
+    _check_here(codes, scales, out)
+    rows = shape[0] * shape[1] if len(shape) == 3 else shape[0]
+    _check(lib().fff_mx4_dequantize(_ptr(codes), _ptr(scales), _ptr(out), _stream_handle(stream), rows, shape[-1], _dtype_code(out)), where)
+
+
+def fff_mx4_product(a, w_codes, w_scales, out, a_scales=None, bias=None, act=ACT_NONE, stream=None) -> None:
+    """out [T, N] = act(A W^T + bias) with W [N, K] in four bits; a [T, K] bfloat16, or with a_scales the codes of such rows.  K is
+    that of a in bfloat16; of codes, what their whole blocks hold (the codes behind a row's end are zeros)."""
+    import torch
+    where = "fff_mx4_product"
+    T, K = _size(where, "a", a, (2,))
+    N = _size(where, "out", out, (2,))[1]
+    if a_scales is not None:
+        K = 32 * _size(where, "a_scales", a_scales, (2,))[1]
+        _expect(where, "a", a, (T, K // 2), torch.uint8)
+        _expect(where, "a_scales", a_scales, (T, K // 32), torch.uint8)
+    elif a.dtype != torch.bfloat16:
+        raise FffError(ERR_DTYPE, where, "a is %s, expected torch.bfloat16, or codes with their scales" % a.dtype)
+    _expect(where, "w_codes", w_codes, (N, 16 * _mx4_blocks(K)), torch.uint8)
+    _expect(where, "w_scales", w_scales, (N, _mx4_blocks(K)), torch.uint8)
+    _expect(where, "out", out, (T, N), out.dtype)
+    _expect(where, "bias", bias, (N,), out.dtype)
+    _check_here(a, a_scales, w_codes, w_scales, bias, out)
+    need, scratch = 0, None
+    if a_scales is None and (K % 8 or a.data_ptr() % 16):
+        need = fff_mx4_product_scratch_bytes(T, K)
+        scratch = _scratch(where, need, stream) if need else None
+    _check(lib().fff_mx4_product(_ptr(a), _ptr(a_scales), _ptr(w_codes), _ptr(w_scales), _ptr(bias), act, _ptr(out), _stream_handle(stream),
+                                 T, K, N, _dtype_code(out), _ptr(scratch), need), where)
+
+
+def fff_mx4_product_scratch_bytes(T: int, K: int) -> int:
+    return int(lib().fff_mx4_product_scratch_bytes(T, K))
+
+
+def fff_leaf_forward_mx4(x, leaf_w1, leaf_s1, leaf_b1, leaf_w2, leaf_s2, leaf_b2, leaf_idx, weight, act, out, stream=None) -> None:
+    """out [T, O] = the networks of the leaves leaf_idx [T, k] (or [T]) of every token of x [T, D], with their matrices in four bits, times
+    weight [T, k] (or [T]; None: ones) and added up.  leaf_w1, leaf_s1 are codes and scales of [leaves, width, D], leaf_w2, leaf_s2
+    of [leaves, O, width]; leaf_b1 [leaves, width]; leaf_b2 [leaves, O]."""
+    import torch
+    where = "fff_leaf_forward_mx4"
+    T, D = _rows(where, "x", x)
+    O = _rows(where, "out", out)[1]
+    E, width = _size(where, "leaf_b1", leaf_b1, (2,))
+    idx_shape = _size(where, "leaf_idx", leaf_idx, (1, 2))
+    k = idx_shape[1] if len(idx_shape) == 2 else 1
+    _expect(where, "leaf_idx", leaf_idx, (T,) + idx_shape[1:], torch.int32)
+    _expect(where, "weight", weight, idx_shape, torch.float32)
+    for name, t, shape, dtype in (("leaf_w1", leaf_w1, (E, width, 16 * _mx4_blocks(D)), torch.uint8),
+                                  ("leaf_s1", leaf_s1, (E, width, _mx4_blocks(D)), torch.uint8), ("leaf_b1", leaf_b1, (E, width), x.dtype),
+                                  ("leaf_w2", leaf_w2, (E, O, 16 * _mx4_blocks(width)), torch.uint8),
+                                  ("leaf_s2", leaf_s2, (E, O, _mx4_blocks(width)), torch.uint8), ("leaf_b2", leaf_b2, (E, O), x.dtype),
+                                  ("out", out, (T, O), x.dtype)):
+        _expect(where, name, t, shape, dtype)
+    _check_here(x, leaf_w1, leaf_s1, leaf_b1, leaf_w2, leaf_s2, leaf_b2, leaf_idx, weight, out)
+    need = fff_leaf_mx4_scratch_bytes(T, D, O, E, k, width)
+    scratch = _scratch(where, need, stream) if need else None
+    _check(lib().fff_leaf_forward_mx4(_ptr(x), _ptr(leaf_w1), _ptr(leaf_s1), _ptr(leaf_b1), _ptr(leaf_w2), _ptr(leaf_s2), _ptr(leaf_b2),
+                                      _ptr(leaf_idx), _ptr(weight), E, k, width, act, _ptr(out), _stream_handle(stream), T, D, O,
+                                      _dtype_code(x), _ptr(scratch), need), where)
+
+
+def fff_leaf_mx4_scratch_bytes(T: int, D: int, O: int, n_leaves: int, k: int, leaf_width: int) -> int:
+    return int(lib().fff_leaf_mx4_scratch_bytes(T, D, O, n_leaves, k, leaf_width))
 
 
 def fff_forward_soft(x, node_w, node_b, leaf_w1, leaf_b1, leaf_w2, leaf_b2, depth, leaf_width, act, out,

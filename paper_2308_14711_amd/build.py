@@ -19,10 +19,10 @@ PROBE_LIB = os.path.join(HERE, "libfff_bench_probes.so")   # measuring sticks of
 OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["fff_api.hip", "fff_walk.hip", "fff_walk_wave.hip", "fff_bucket.hip", "fff_leaf.hip", "fff_leaf_tiles.hip", "fff_leaf_slices.hip", "fff_subtree.hip",
-           "fff_token_block.hip", "fff_token_rows.hip", "fff_moe_gate.hip", "fff_soft.hip", "fff_block.hip"]
+           "fff_token_block.hip", "fff_token_rows.hip", "fff_moe_gate.hip", "fff_soft.hip", "fff_block.hip", "fff_mx4.hip", "fff_mx4_product.hip", "fff_moe_route.hip"]
 PROBE_SOURCES = ["bench_probes.hip"]
 TORCH_SOURCE = "fff_torch.cpp"
-HEADERS = ["fff_device.h", "fff_internal.h", "fff_mfma_tile.h", os.path.join("..", "..", "include", "fff.h")]
+HEADERS = ["fff_device.h", "fff_internal.h", "fff_mfma_tile.h", "fff_mx4.h", os.path.join("..", "..", "include", "fff.h")]
 
 # packed fp32 VALU forms are switched off on purpose: some of them have given wrong results on
 # the target machines; ordinary float code is compiled without them

@@ -5,12 +5,14 @@
 
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
 
 #include "../../include/fff.h"
 #include "fff_internal.h"
+#include "fff_mx4.h"
 
 // Scratch of fff_forward_hard_static, the entry point for callers that cannot allocate: a fixed
 // block in the device image of this library, so every GPU the library runs on holds one copy of it
@@ -1068,6 +1070,219 @@ int fff_moe_top1_forward(const void* x, const void* gate_w, const void* gate_b, 
     }
     g_opt.last_path = kPathStaged;
     return run_leaf_stage(p, ei, ws, s, subtree_levels(p, true) == 0, true);
+}
+
+// ---- operators around routed experts and four-bit matrices --------------------------------------------------
+
+// The host checks of scratch that a call uses.
+static int check_scratch(const void* scratch, size_t bytes, size_t need) {
+    if (!scratch) return FFF_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return FFF_ERR_WORKSPACE;
+    if (bytes < need) {
+        g_last_error = "the scratch holds " + std::to_string(bytes) + " bytes, this call needs " + std::to_string(need);
+        return FFF_ERR_WORKSPACE;
+    }
+    return FFF_OK;
+}
+
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Memory that a call reads or writes.
+struct Span {
+    const void* p;
+    int64_t bytes;
+};
+// Whether `w` overlaps one of the others (those without memory aside).
+static bool overlaps_any(const Span& w, std::initializer_list<Span> others) {
+    if (!w.p) return false;
+    for (const Span& o : others)
+        if (o.p && overlaps(w.p, w.bytes, o.p, o.bytes)) return true;
+    return false;
+}
+
+static int check_route(int64_t n_experts, int k, int64_t T, int dtype) {
+    if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
+    if (T < 0 || T > kMaxTokens || n_experts < 1 || n_experts > kMaxExperts || k < 1 || k > kMaxChoices || k > n_experts) return FFF_ERR_RANGE;
+    if (T * k > kMaxTokens) return FFF_ERR_RANGE;
+    if (T * n_experts > kMaxElems) return FFF_ERR_SHAPE;
+    return FFF_OK;
+}
+
+int fff_moe_route(const void* logits, const uint8_t* token_mask, int64_t n_experts, int k, int normalise, int32_t* expert_idx,
+                  float* weight, int32_t* count, float* prob_mean, float* loss, void* stream, int64_t T, int dtype, void* scratch,
+                  size_t scratch_bytes) {
+    int rc = check_route(n_experts, k, T, dtype);
+    if (rc != FFF_OK) return rc;
+    const bool stats = count || prob_mean || loss;
+    if (T == 0 && !stats) return FFF_OK;
+    if (T > 0) {
+        if (!logits || !expert_idx || !weight) return FFF_ERR_NULL;
+        const size_t need = stats ? (size_t)route_scratch_bytes(T, n_experts) : 0;
+        if (stats && (rc = check_scratch(scratch, scratch_bytes, need)) != FFF_OK) return rc;
+        const Span out[] = {{expert_idx, T * k * 4}, {weight, T * k * 4}, {count, (n_experts + 1) * 4}, {prob_mean, n_experts * 4}, {loss, 8},
+                            {stats ? scratch : nullptr, (int64_t)need}};
+        const Span in[] = {{logits, T * n_experts * (dtype == FFF_BF16 ? 2 : 4)}, {token_mask, T}};
+        for (int i = 0; i < 6; ++i) {
+            if (overlaps_any(out[i], {in[0], in[1]})) return FFF_ERR_ALIAS;
+            for (int j = 0; j < i; ++j)
+                if (overlaps_any(out[i], {out[j]})) return FFF_ERR_ALIAS;
+        }
+    }
+    begin_device_call();
+    const Route r{logits, token_mask, T, n_experts, k, normalise != 0, dtype == FFF_BF16};
+    const hipError_t e = launch_route(r, expert_idx, weight, count, prob_mean, loss, scratch, (hipStream_t)stream);
+    return e == hipSuccess ? FFF_OK : set_device_error(e, "routing kernel launch");
+}
+
+size_t fff_route_scratch_bytes(int64_t T, int64_t n_experts) {
+    return check_route(n_experts, 1, T, FFF_F32) == FFF_OK ? (size_t)route_scratch_bytes(T, n_experts) : 0;
+}
+
+int fff_moe_route_backward(const void* logits, const uint8_t* token_mask, int64_t n_experts, int k, int normalise,
+                           const int32_t* expert_idx, const int32_t* count, const float* dweight, const float* dloss, void* dlogits,
+                           void* stream, int64_t T, int dtype) {
+    const int rc = check_route(n_experts, k, T, dtype);
+    if (rc != FFF_OK) return rc;
+    if (T == 0) return FFF_OK;
+    if (!logits || !dlogits || (dweight && !expert_idx) || (dloss && !count)) return FFF_ERR_NULL;
+    const int64_t bytes = T * n_experts * (dtype == FFF_BF16 ? 2 : 4);
+    if (overlaps_any({dlogits, bytes}, {{logits, bytes}, {token_mask, T}, {expert_idx, T * k * 4}, {count, (n_experts + 1) * 4}, {dweight, T * k * 4},
+                                        {dloss, 8}}))
+        return FFF_ERR_ALIAS;
+    begin_device_call();
+    const Route r{logits, token_mask, T, n_experts, k, normalise != 0, dtype == FFF_BF16};
+    const hipError_t e = launch_route_backward(r, expert_idx, count, dweight, dloss, dlogits, (hipStream_t)stream);
+    return e == hipSuccess ? FFF_OK : set_device_error(e, "routing gradient kernel launch");
+}
+
+int fff_mx4_quantize(const void* src, uint8_t* codes, uint8_t* scales, int transpose, void* stream, int64_t batch, int64_t rows,
+                     int64_t cols, int dtype) {
+    if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
+    if (batch < 0 || batch > kMaxElems) return FFF_ERR_RANGE;
+    if (rows < 1 || cols < 1 || rows > kMaxElems || cols > kMaxElems / rows) return FFF_ERR_SHAPE;
+    if (batch == 0) return FFF_OK;
+    // (blocks of 32 and tiles of columns count whole: 2^40 of either is the limit too)
+    if (batch > kMaxElems / (rows * cols) || batch * (transpose ? cols : rows) > (kMaxElems >> 5) / mx_blocks(transpose ? rows : cols)) return FFF_ERR_SHAPE;
+    if (transpose && batch > (((int64_t)1 << 31) - 1) / (((rows + 127) / 128) * ((cols + 63) / 64))) return FFF_ERR_SHAPE;
+    if (!src || !codes || !scales) return FFF_ERR_NULL;
+    if (!aligned16(codes)) return FFF_ERR_UNSUPPORTED;
+    const int64_t blocks = batch * (transpose ? cols * mx_blocks(rows) : rows * mx_blocks(cols));
+    const Span s{src, batch * rows * cols * (dtype == FFF_BF16 ? 2 : 4)}, c{codes, 16 * blocks}, b{scales, blocks};
+    if (overlaps_any(c, {s, b}) || overlaps_any(b, {s})) return FFF_ERR_ALIAS;
+    begin_device_call();
+    const hipError_t e = launch_mx4_quantize(src, codes, scales, transpose != 0, batch, rows, cols, dtype == FFF_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? FFF_OK : set_device_error(e, "quantisation kernel launch");
+}
+
+int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, void* stream, int64_t rows, int64_t cols, int dtype) {
+    if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
+    if (rows < 0 || rows > kMaxElems) return FFF_ERR_RANGE;
+    if (cols < 1 || cols > kMaxElems || (rows > 0 && mx_blocks(cols) > (kMaxElems >> 5) / rows)) return FFF_ERR_SHAPE;
+    if (rows == 0) return FFF_OK;
+    if (!codes || !scales || !out) return FFF_ERR_NULL;
+    if (!aligned16(codes)) return FFF_ERR_UNSUPPORTED;
+    if (overlaps_any({out, rows * cols * (dtype == FFF_BF16 ? 2 : 4)}, {{codes, 16 * rows * mx_blocks(cols)}, {scales, rows * mx_blocks(cols)}}))
+        return FFF_ERR_ALIAS;
+    begin_device_call();
+    const hipError_t e = launch_mx4_dequantize(codes, scales, out, rows, cols, dtype == FFF_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? FFF_OK : set_device_error(e, "dequantisation kernel launch");
+}
+
+static constexpr int64_t kMaxMx4Side = (int64_t)1 << 24;
+
+// bf16 rows of whole aligned pieces of 16 bytes are read where they are, others from a copy in scratch
+static bool rows_as_they_are(const void* a, int64_t K) { return K % 8 == 0 && aligned16(a); }
+static size_t padded_rows_bytes(int64_t T, int64_t K) { return ((size_t)(T * mx_blocks(K) * 2 * kMxBlock) + 255) / 256 * 256; }
+
+int fff_mx4_product(const void* a, const uint8_t* a_scales, const uint8_t* w, const uint8_t* w_scales, const void* bias, int act,
+                    void* out, void* stream, int64_t T, int64_t K, int64_t N, int dtype, void* scratch, size_t scratch_bytes) {
+    if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
+    if (T < 0 || T > kMaxTokens) return FFF_ERR_RANGE;
+    if (K < 1 || N < 1 || K > kMaxMx4Side || N > kMaxMx4Side || T * mx_blocks(K) > (kMaxElems >> 5) || T * N > kMaxElems ||
+        N * mx_blocks(K) > (kMaxElems >> 5))
+        return FFF_ERR_SHAPE;
+    if (act != FFF_ACT_RELU && act != FFF_ACT_GELU && act != FFF_ACT_NONE) return FFF_ERR_UNSUPPORTED;
+    if (!a_scales && dtype != FFF_BF16) return FFF_ERR_UNSUPPORTED;
+    if (T == 0) return FFF_OK;
+    if (!a || !w || !w_scales || !out) return FFF_ERR_NULL;
+    if (!aligned16(w) || (a_scales && !aligned16(a))) return FFF_ERR_UNSUPPORTED;
+    const int64_t es = dtype == FFF_BF16 ? 2 : 4, Kb = mx_blocks(K);
+    const bool pad = !a_scales && !rows_as_they_are(a, K);
+    const size_t need = pad ? padded_rows_bytes(T, K) : 0;
+    if (pad) {
+        const int rc = check_scratch(scratch, scratch_bytes, need);
+        if (rc != FFF_OK) return rc;
+    }
+    const Span in_a{a, a_scales ? 16 * T * Kb : T * K * 2}, in_s{a_scales, T * Kb}, in_w{w, 16 * N * Kb}, in_ws{w_scales, N * Kb}, in_b{bias, N * es};
+    const Span o{out, T * N * es}, sc{pad ? scratch : nullptr, (int64_t)need};
+    if (overlaps_any(o, {in_a, in_s, in_w, in_ws, in_b, sc}) || overlaps_any(sc, {in_a, in_w, in_ws, in_b})) return FFF_ERR_ALIAS;
+    begin_device_call();
+    const hipStream_t s = (hipStream_t)stream;
+    Mx4Product p{a, a_scales, K, w, w_scales, bias, out, T, K, N, act, dtype == FFF_BF16};
+    hipError_t e = hipSuccess;
+    if (pad) {
+        e = launch_pad_rows((const uint16_t*)a, (uint16_t*)scratch, T, K, s);
+        p.a = scratch;
+        p.lda = Kb * kMxBlock;
+    }
+    if (e == hipSuccess) e = launch_mx4_product(p, s);
+    return e == hipSuccess ? FFF_OK : set_device_error(e, "four-bit product kernel launch");
+}
+
+size_t fff_mx4_product_scratch_bytes(int64_t T, int64_t K) {
+    return T < 1 || T > kMaxTokens || K < 1 || K > kMaxMx4Side || T * mx_blocks(K) > (kMaxElems >> 5) ? 0 : padded_rows_bytes(T, K);
+}
+
+static int check_leaf_mx4(int64_t T, int64_t D, int64_t O, int64_t n_leaves, int k, int leaf_width) {
+    if (T < 0 || T > kMaxTokens || k < 1 || k > kMaxChoices || T * k > kMaxTokens || n_leaves < 1 || n_leaves > 65536 || leaf_width < 1 ||
+        leaf_width > 65536)
+        return FFF_ERR_RANGE;
+    if (D < 1 || O < 1 || D > kMaxMx4Side || O > kMaxMx4Side) return FFF_ERR_SHAPE;
+    const int64_t rows = T * k > n_leaves ? T * k : n_leaves;
+    const int64_t m = (D > O ? D : O) + kMxBlock, l = leaf_width + kMxBlock;
+    if (m > kMaxElems / rows || l > kMaxElems / rows || n_leaves * l > kMaxElems / m) return FFF_ERR_SHAPE;
+    return FFF_OK;
+}
+
+size_t fff_leaf_mx4_scratch_bytes(int64_t T, int64_t D, int64_t O, int64_t n_leaves, int k, int leaf_width) {
+    if (check_leaf_mx4(T, D, O, n_leaves, k, leaf_width) != FFF_OK || T == 0) return 0;
+    return (size_t)mx4_leaves_scratch_bytes(T, O, n_leaves, k, leaf_width) + padded_rows_bytes(T, D);
+}
+
+int fff_leaf_forward_mx4(const void* x, const uint8_t* leaf_w1, const uint8_t* leaf_s1, const void* leaf_b1, const uint8_t* leaf_w2,
+                         const uint8_t* leaf_s2, const void* leaf_b2, const int32_t* leaf_idx, const float* weight, int64_t n_leaves,
+                         int k, int leaf_width, int act, void* out, void* stream, int64_t T, int64_t D, int64_t O, int dtype,
+                         void* scratch, size_t scratch_bytes) {
+    if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
+    int rc = check_leaf_mx4(T, D, O, n_leaves, k, leaf_width);
+    if (rc != FFF_OK) return rc;
+    if (dtype != FFF_BF16 || (act != FFF_ACT_RELU && act != FFF_ACT_GELU)) return FFF_ERR_UNSUPPORTED;
+    if (T == 0) return FFF_OK;
+    if (!x || !leaf_w1 || !leaf_s1 || !leaf_b1 || !leaf_w2 || !leaf_s2 || !leaf_b2 || !leaf_idx || !out) return FFF_ERR_NULL;
+    if (!aligned16(leaf_w1) || !aligned16(leaf_w2)) return FFF_ERR_UNSUPPORTED;
+    const size_t need = fff_leaf_mx4_scratch_bytes(T, D, O, n_leaves, k, leaf_width);
+    if ((rc = check_scratch(scratch, scratch_bytes, need)) != FFF_OK) return rc;
+    const int64_t n1 = n_leaves * leaf_width, n2 = n_leaves * O, P = T * k;
+    const Span in[] = {{x, T * D * 2}, {leaf_w1, 16 * n1 * mx_blocks(D)}, {leaf_s1, n1 * mx_blocks(D)}, {leaf_b1, 2 * n1},
+                       {leaf_w2, 16 * n2 * mx_blocks(leaf_width)}, {leaf_s2, n2 * mx_blocks(leaf_width)}, {leaf_b2, 2 * n2}, {leaf_idx, 4 * P},
+                       {weight, 4 * P}};
+    const Span o{out, T * O * 2}, sc{scratch, (int64_t)need};
+    for (const Span& i : in)
+        if (overlaps_any(i, {o, sc})) return FFF_ERR_ALIAS;
+    if (overlaps_any(o, {sc})) return FFF_ERR_ALIAS;
+    begin_device_call();
+    const hipStream_t s = (hipStream_t)stream;
+    Mx4Leaves p{(const uint16_t*)x, D, leaf_w1, leaf_s1, leaf_w2, leaf_s2, (const uint16_t*)leaf_b1, (const uint16_t*)leaf_b2, leaf_idx, weight,
+                (uint16_t*)out, T, D, O, n_leaves, k, leaf_width, act};
+    hipError_t e = hipSuccess;
+    if (!rows_as_they_are(x, D)) {
+        uint16_t* const copy = (uint16_t*)((char*)scratch + mx4_leaves_scratch_bytes(T, O, n_leaves, k, leaf_width));
+        e = launch_pad_rows((const uint16_t*)x, copy, T, D, s);
+        p.x = copy;
+        p.ldx = mx_blocks(D) * kMxBlock;
+    }
+    if (e == hipSuccess) e = launch_mx4_leaves(p, scratch, s);
+    return e == hipSuccess ? FFF_OK : set_device_error(e, "four-bit leaf kernel launch");
 }
 
 int fff_forward_soft(const void* x, const void* node_w, const void* node_b, const void* leaf_w1,
