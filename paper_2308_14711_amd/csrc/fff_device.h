@@ -199,6 +199,20 @@ __device__ __forceinline__ int64_t xcd_contiguous_block() {
     return (int64_t)(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;
 }
 
+// 16 bytes a lane straight to LDS: lane i's land at lds + 16 i.  Written as assembly because the compiler
+// waits for every such load before any LDS access that follows it; the waits are wait_loads' below.  (m0 is never allocated
+// to a value of the program, and nothing else in these kernels needs it.)
+__device__ __forceinline__ void load_to_lds(const char* src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
+}
+// until at most N of this wave's loads are outstanding (they return in order)
+template <int N> __device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
 // Slot (16 bytes) of piece c of row r in an LDS tile of 128-byte rows that MFMA operands are read
 // from: 8 r + ((c + rot(r)) mod 8), rot(r) = bit 1 of r + 4 * bit 2 of r.
 //

@@ -249,6 +249,232 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(const Args a) {
     }
 }
 
+// ---- tiles through LDS -------------------------------------------------------------------------------------
+//
+// Many rows of A: a block of WM x WN waves takes 16 MT WM rows of A against 16 NT WN rows of W, a wave 16 MT x 16 NT results.  A stage is 128
+// elements of K (bf16 rows: 256 bytes of a row of A, 64 of W) or 256 (codes: 128 bytes of either); two stages, one on its way
+// straight to LDS while the other is multiplied.  Scale bytes go to registers, a stage ahead too.
+//
+// Pieces of 16 bytes in LDS are turned within their row so that the 16 lanes of a pass of an operand read (rows
+// {0-3, 12-15} of one g with rows {4-11} of its neighbour, then the others) meet every bank once; the turn is made by
+// the lanes' source addresses, since a load to LDS writes lane after lane:
+//   128-byte rows, pieces 2 g + u: tile_swz's; 256-byte rows, pieces 4 g + u: (row & 3) + 8 (row >> 3 & 1) further; 64-byte rows, piece g:
+//   2 (row >> 3 & 1) further.
+__device__ const uint4 g_zero_piece = {0, 0, 0, 0};
+
+template <int ROW> __device__ __forceinline__ int turn(int row) {
+    return ROW == 256 ? (row & 3) + 8 * ((row >> 3) & 1) : ROW == 128 ? lds_rot(row) : 2 * ((row >> 3) & 1);
+}
+template <int ROW> __device__ __forceinline__ int lds_slot(int row, int piece) {
+    constexpr int n = ROW / 16;
+    return row * n + ((piece + turn<ROW>(row)) & (n - 1));
+}
+
+// `count` scale bytes of a row from block b on, the first in the low byte; zeros behind the row's Kb
+template <int COUNT> __device__ __forceinline__ uint32_t load_scales(const uint8_t* row, int b, int Kb) {
+    typedef uint32_t u32_any __attribute__((aligned(1)));
+    typedef uint16_t u16_any __attribute__((aligned(1)));
+    if (b + COUNT <= Kb) return COUNT == 4 ? *(const u32_any*)(row + b) : (uint32_t) * (const u16_any*)(row + b);
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+        if (b + i < Kb) v |= (uint32_t)row[b + i] << (8 * i);
+    return v;
+}
+
+template <bool A4, int WM, int WN, int MT, int NT> struct TileShape {
+    static constexpr int kThreads = 64 * WM * WN, kWaves = WM * WN, kRows = 16 * MT * WM, kCols = 16 * NT * WN;
+    static constexpr int kARow = A4 ? 128 : 256, kWRow = A4 ? 128 : 64;         // bytes of a row in a stage
+    static constexpr int kStepBlocks = A4 ? 8 : 4;                                // blocks of 32 in a stage
+    static constexpr int kABytes = kRows * kARow, kWBytes = kCols * kWRow, kStage = kABytes + kWBytes;
+    static constexpr int kALoads = kABytes / 1024 / kWaves, kWLoads = kWBytes / 1024 / kWaves;   // a wave's loads of 1 KB a stage
+    static_assert(kALoads * 1024 * kWaves == kABytes && kWLoads * 1024 * kWaves == kWBytes, "whole loads a wave");
+};
+
+template <bool A4, int MODE, int WM, int WN, int MT, int NT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mx4_tile_kernel(const Args a, const int64_t row_tiles, const int64_t col_tiles) {
+    typedef TileShape<A4, WM, WN, MT, NT> S;
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = lane & 15, g = lane >> 4;
+    const int wm = wv / WN, wn = wv % WN;
+    // an XCD takes a contiguous range of tiles, eight row tiles against all columns at a time
+    const int64_t id = xcd_contiguous_block();
+    if (id >= row_tiles * col_tiles) return;
+    const int64_t group = id / (8 * col_tiles), in = id - group * 8 * col_tiles;
+    const int64_t tall = row_tiles - 8 * group < 8 ? row_tiles - 8 * group : 8;
+    const int64_t rt = 8 * group + in % tall, ct = in / tall;
+    const int64_t n0 = ct * S::kCols;
+    int64_t leaf = 0, first, rows;
+    if constexpr (MODE == kDense) {
+        first = rt * S::kRows;
+        rows = a.T - first;
+    } else {
+        if (rt >= *a.n_tiles) return;
+        leaf = a.tile_leaf[rt];
+        first = a.tile_slot[rt];
+        rows = a.start[leaf + 1] - first;
+    }
+    if (rows > S::kRows) rows = S::kRows;
+    const auto a_index = [&](int64_t r) -> int64_t {
+        r = (r < rows ? r : rows - 1) + first;
+        if constexpr (MODE == kHidden) r = a.perm[r] / a.k;
+        return r;
+    };
+    const auto w_index = [&](int64_t n) -> int64_t { return leaf * a.N + (n0 + n < a.N ? n0 + n : a.N - 1); };
+    const int64_t w_row_bytes = (int64_t)a.Kb * 16;
+
+    // sources of this lane's pieces: piece `p` of its rows in stage 0
+    const char* a_src[S::kALoads];
+    const char* w_src[S::kWLoads];
+    int a_piece[S::kALoads], w_piece[S::kWLoads];
+#pragma unroll
+    for (int i = 0; i < S::kALoads; ++i) {
+        constexpr int n = S::kARow / 16;
+        const int row = (i * S::kWaves + wv) * (64 / n) + lane / n;
+        a_piece[i] = (lane - turn<S::kARow>(row)) & (n - 1);
+        a_src[i] = a.a + a_index(row) * a.a_row + 16 * a_piece[i];
+    }
+#pragma unroll
+    for (int i = 0; i < S::kWLoads; ++i) {
+        constexpr int n = S::kWRow / 16;
+        const int row = (i * S::kWaves + wv) * (64 / n) + lane / n;
+        w_piece[i] = (lane - turn<S::kWRow>(row)) & (n - 1);
+        w_src[i] = (const char*)a.w + w_index(row) * w_row_bytes + 16 * w_piece[i];
+    }
+    // rows of scales of this lane's operands
+    const uint8_t* ws_row[NT];
+    const uint8_t* as_row[MT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) ws_row[n] = a.w_scales + w_index(16 * (wn * NT + n) + j) * a.Kb;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) as_row[m] = A4 ? a.a_scales + a_index(16 * (wm * MT + m) + j) * a.Kb : nullptr;
+
+    const int stages = (a.Kb + S::kStepBlocks - 1) / S::kStepBlocks;
+    const int a_pieces = A4 ? a.Kb : a.pieces;
+    const char* const zero = (const char*)&g_zero_piece;
+    const uint32_t lds0 = lds_address(lds);
+    uint32_t w_scale[NT], a_scale[MT];
+    const auto fetch = [&](int c, int buf) {
+        const int64_t a_off = (int64_t)c * S::kARow, w_off = (int64_t)c * S::kWRow;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) w_scale[n] = A4 ? load_scales<2>(ws_row[n], 8 * c + 2 * g, a.Kb) : load_scales<4>(ws_row[n], 4 * c, a.Kb);
+        if constexpr (A4) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) a_scale[m] = load_scales<2>(as_row[m], 8 * c + 2 * g, a.Kb);
+        }
+        const uint32_t at = lds0 + buf * S::kStage;
+#pragma unroll
+        for (int i = 0; i < S::kALoads; ++i)
+            load_to_lds(c * (S::kARow / 16) + a_piece[i] < a_pieces ? a_src[i] + a_off : zero, __builtin_amdgcn_readfirstlane(at + (i * S::kWaves + wv) * 1024));
+#pragma unroll
+        for (int i = 0; i < S::kWLoads; ++i)
+            load_to_lds(c * (S::kWRow / 16) + w_piece[i] < a.Kb ? w_src[i] + w_off : zero,
+                        __builtin_amdgcn_readfirstlane(at + S::kABytes + (i * S::kWaves + wv) * 1024));
+    };
+
+    f32x4_t acc[NT][MT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+    fetch(0, 0);
+    for (int c = 0; c < stages; ++c) {
+        // the stage is there (this wave's part, then everybody's), and nobody reads the other buffer any more
+        wait_loads<0>();
+        uint32_t ws[NT], as[MT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) ws[n] = w_scale[n];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(ws[n]));      // (the compiler waits for its loads here, not behind the next stage's)
+        if constexpr (A4) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) as[m] = a_scale[m];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) asm volatile("" : "+v"(as[m]));
+        }
+        __syncthreads();
+        if (c + 1 < stages) fetch(c + 1, (c + 1) & 1);
+        const uint4* const la = (const uint4*)(lds + (c & 1) * S::kStage);
+        const uint4* const lw = (const uint4*)(lds + (c & 1) * S::kStage + S::kABytes);
+        if constexpr (A4) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint4 fa[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) fa[m] = la[lds_slot<128>(16 * (wm * MT + m) + j, 2 * g + u)];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 fw = lw[lds_slot<128>(16 * (wn * NT + n) + j, 2 * g + u)];
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[n][m] = mfma4(fw, u ? ws[n] >> 8 : ws[n], fa[m], u ? as[m] >> 8 : as[m], acc[n][m]);
+                }
+            }
+        } else {
+            uint4 fw[NT];
+            float s[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                fw[n] = lw[lds_slot<64>(16 * (wn * NT + n) + j, g)];
+                s[n] = __uint_as_float(((ws[n] >> (8 * g)) & 255u) << 23);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                bf16x8_t fa[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) fa[m] = __builtin_bit_cast(bf16x8_t, la[lds_slot<256>(16 * (wm * MT + m) + j, 4 * g + u)]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const bf16x8_t f = dequantise8(u == 0 ? fw[n].x : u == 1 ? fw[n].y : u == 2 ? fw[n].z : fw[n].w, s[n]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, fa[m], acc[n][m], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int64_t row = 16 * (wm * MT + m) + j;
+        if (row >= rows) continue;
+        int64_t to = first + row;
+        float scale = 1.0f;
+        if constexpr (MODE == kOutput) {
+            to = a.perm[to];
+            if (a.k == 1 && a.weight) scale = a.weight[to];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int64_t n4 = n0 + 16 * (wn * NT + n) + 4 * g;
+            const int64_t limit = MODE == kHidden ? a.out_row : a.N;
+            if (n4 >= limit) continue;
+            float o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float v = acc[n][m][q];
+                if constexpr (MODE == kDense) o[q] = n4 + q < a.N ? apply(v + bias_at(a, a.bias, n4 + q), a.act) : 0.f;
+                else if constexpr (MODE == kHidden) o[q] = n4 + q < a.N ? apply(v + bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n4 + q]), a.act) : 0.f;
+                else o[q] = n4 + q < a.N ? (v + bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n4 + q])) * scale : 0.f;
+            }
+            store4(a.out, MODE == kHidden || a.out_bf16, MODE == kHidden || a.out_vec, to * a.out_row, n4, limit, o);
+        }
+    }
+}
+
+template <bool A4, int MODE, int WM, int WN, int MT, int NT> hipError_t launch_tiles(const Args& a, int64_t row_tiles, hipStream_t s) {
+    typedef TileShape<A4, WM, WN, MT, NT> S;
+    const int64_t width = MODE == kHidden ? a.out_row : a.N;
+    const int64_t col_tiles = (width + S::kCols - 1) / S::kCols;
+    const int64_t blocks = (row_tiles * col_tiles + kXcds - 1) / kXcds * kXcds;
+    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    note_launch("mx4_tile_kernel<%s,%d,%d,%s>", A4 ? "mx4" : "bf16", S::kRows, S::kCols, MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : "output");
+    const auto kernel = mx4_tile_kernel<A4, MODE, WM, WN, MT, NT>;
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * S::kStage);
+    if (e != hipSuccess) return e;
+    kernel<<<dim3((unsigned)blocks), S::kThreads, 2 * S::kStage, s>>>(a, row_tiles, col_tiles);
+    return hipGetLastError();
+}
+
 // ---- grouping of the pairs by leaf -------------------------------------------------------------------------
 //
 // rank[p] = place of pair p among its leaf's; which pair gets which place depends on the order of the atomics, and
@@ -396,6 +622,10 @@ hipError_t launch_mx4_product(const Mx4Product& p, hipStream_t s) {
     a.act = p.act;
     a.out_bf16 = p.out_bf16;
     a.out_vec = p.N % 4 == 0 && ((uintptr_t)p.out & (p.out_bf16 ? 7 : 15)) == 0;
+    if (p.T >= 128) {
+        if (a4) return launch_tiles<true, kDense, 2, 4, 4, 4>(a, (p.T + 127) / 128, s);
+        return launch_tiles<false, kDense, 2, 4, 4, 4>(a, (p.T + 127) / 128, s);
+    }
     const int mt = rows_tile(p.T);
     const int64_t tiles = (p.T + 16 * mt - 1) / (16 * mt);
     return a4 ? launch_rows<true, kDense>(a, tiles, mt, s) : launch_rows<false, kDense>(a, tiles, mt, s);
@@ -445,8 +675,9 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
         if ((e = launch_rows<false, kHiddenDirect>(a, P, 1, s)) != hipSuccess) return e;
         return launch_rows<false, kOutputDirect>(b, p.T, 1, s);
     }
+    const bool large = P / p.E >= 64;
     const int mt = rows_tile(P / p.E);
-    const int tile_rows = 16 * mt;
+    const int tile_rows = large ? 128 : 16 * mt;
     const int64_t tiles = P / tile_rows + (p.E < P ? p.E : P);
     int32_t *const count = words(at.count), *const start = words(at.start), *const tile_start = words(at.tile_start);
     int32_t *const rank = words(at.rank), *const perm = words(at.perm), *const tile_leaf = words(at.tile_leaf), *const tile_slot = words(at.tile_slot);
@@ -468,8 +699,13 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
         b.out_bf16 = false;
         b.out_vec = p.O % 4 == 0;
     }
-    if ((e = launch_rows<false, kHidden>(a, tiles, mt, s)) != hipSuccess) return e;
-    if ((e = launch_rows<false, kOutput>(b, tiles, mt, s)) != hipSuccess) return e;
+    if (large) {
+        if ((e = launch_tiles<false, kHidden, 2, 4, 4, 4>(a, tiles, s)) != hipSuccess) return e;
+        if ((e = launch_tiles<false, kOutput, 2, 4, 4, 4>(b, tiles, s)) != hipSuccess) return e;
+    } else {
+        if ((e = launch_rows<false, kHidden>(a, tiles, mt, s)) != hipSuccess) return e;
+        if ((e = launch_rows<false, kOutput>(b, tiles, mt, s)) != hipSuccess) return e;
+    }
     note_launch("combine_kernel");
     combine_kernel<<<dim3((unsigned)p.T), 256, 0, s>>>(p.idx, p.weight, y, p.out, p.T, p.O, p.E, p.k);
     return hipGetLastError();

@@ -102,20 +102,6 @@ __device__ __forceinline__ Tile find_tile(const int32_t* __restrict__ offset, in
     return Tile{g, first, end - first < kTok ? end - first : kTok};
 }
 
-// 16 bytes a lane straight to LDS: lane i's land at lds + 16 i.  Written as assembly because the compiler
-// waits for every such load before any LDS access that follows it; the waits are wait_loads' below.  (m0 is never allocated
-// to a value of the program, and nothing else in these kernels needs it.)
-__device__ __forceinline__ void load_to_lds(const char* src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
-}
-// until at most N of this wave's loads are outstanding (they return in order)
-template <int N> __device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-
 template <bool BF16>
 __device__ __forceinline__ f32x4_t mfma_piece(const uint4& w, const uint4& x, f32x4_t acc) {
     if (BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, x), acc, 0, 0, 0);
