@@ -280,7 +280,7 @@ int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, v
  *   scratch   device memory, 256-byte aligned, of one call until its launches have run, at least
  *             fff_mx4_product_scratch_bytes: a copy of bf16 rows that are not whole aligned pieces of 16 bytes (K not a
  *             multiple of 8, or a misaligned); never read otherwise, and may be NULL then
- * K <= 2^24, N <= 2^24.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T), FFF_ERR_SHAPE, FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (act, or misaligned codes),
+ * K <= 2^22, N <= 2^22.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T), FFF_ERR_SHAPE, FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (act, or misaligned codes),
  * FFF_ERR_ALIAS (out or scratch overlaps an input or each other), FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.
  */
 int fff_mx4_product(const void* a, const uint8_t* a_scales, const uint8_t* w, const uint8_t* w_scales,

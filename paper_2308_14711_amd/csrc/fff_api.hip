@@ -1188,7 +1188,7 @@ int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, v
     return e == hipSuccess ? FFF_OK : set_device_error(e, "dequantisation kernel launch");
 }
 
-static constexpr int64_t kMaxMx4Side = (int64_t)1 << 24;
+static constexpr int64_t kMaxMx4Side = (int64_t)1 << 22;
 
 // bf16 rows of whole aligned pieces of 16 bytes are read where they are, others from a copy in scratch
 static bool rows_as_they_are(const void* a, int64_t K) { return K % 8 == 0 && aligned16(a); }

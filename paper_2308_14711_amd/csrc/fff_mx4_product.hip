@@ -10,8 +10,20 @@
 #include "fff_device.h"
 #include "fff_mx4.h"
 
+#include <type_traits>
+
 namespace fff {
 namespace {
+
+// an address that is the same in all lanes, in scalar registers
+__device__ __forceinline__ const char* uniform(const char* p) {
+    const uint64_t v = (uint64_t)p;
+    return (const char*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32);
+}
+// load_to_lds from a base that the wave shares
+__device__ __forceinline__ void load_to_lds_from(const char* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
@@ -55,31 +67,14 @@ __device__ __forceinline__ f32x4_t mfma4(const uint4& w, uint32_t ws, const uint
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, va, acc, 4, 4, 0, (int)ws, 0, (int)as);
 }
 
-// One step of 128 elements: block b of this lane's row of W against MT rows of A.  TAIL: b may lie behind the row's end, and
-// the block may be cut (pieces of bf16 rows): zeros there.
-template <bool A4, int MT, bool TAIL>
-__device__ __forceinline__ void step128(const uint8_t* w_row, const uint8_t* ws_row, const char* const (&a_row)[MT],
-                                        const uint8_t* const (&as_row)[MT], int b, int Kb, int pieces, f32x4_t (&acc)[MT]) {
-    const bool in = !TAIL || b < Kb;
-    const int bb = in ? b : Kb - 1;
-    const uint4 w = keep_if(in, *(const uint4*)(w_row + 16 * (int64_t)bb));
-    const uint32_t ws = in ? ws_row[bb] : 0u;
+// One step of 128 elements: a block of 32 of this lane's row of W against MT rows of A (A in bf16: four pieces each).
+template <bool A4, int MT>
+__device__ __forceinline__ void multiply128(const uint4& w, uint32_t ws, const uint4 (&a)[MT][A4 ? 1 : 4], const uint32_t (&as)[MT], f32x4_t (&acc)[MT]) {
     if constexpr (A4) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const uint4 a = keep_if(in, *(const uint4*)(a_row[m] + 16 * (int64_t)bb));
-            acc[m] = mfma4(w, ws, a, in ? as_row[m][bb] : 0u, acc[m]);
-        }
+        for (int m = 0; m < MT; ++m) acc[m] = mfma4(w, ws, a[m][0], as[m], acc[m]);
     } else {
         const float s = __uint_as_float(ws << 23);
-        uint4 a[MT][4];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int p = 4 * bb + u;
-                a[m][u] = keep_if(in && (!TAIL || p < pieces), *(const uint4*)(a_row[m] + 16 * (int64_t)(!TAIL || p < pieces ? p : 0)));
-            }
         const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -91,16 +86,65 @@ __device__ __forceinline__ void step128(const uint8_t* w_row, const uint8_t* ws_
     }
 }
 
-// The steps wv, wv + waves, ... of the rows' steps.
+// The same with its loads, at a row's end: block b may lie behind it, and the block may be cut (pieces of bf16 rows): zeros there.
+template <bool A4, int MT>
+__device__ __forceinline__ void step128(const uint8_t* w_row, const uint8_t* ws_row, const char* const (&a_row)[MT],
+                                        const uint8_t* const (&as_row)[MT], int b, int Kb, int pieces, f32x4_t (&acc)[MT]) {
+    constexpr int kPieces = A4 ? 1 : 4;
+    const bool in = b < Kb;
+    const int bb = in ? b : Kb - 1;
+    const uint4 w = keep_if(in, *(const uint4*)(w_row + 16 * (int64_t)bb));
+    const uint32_t ws = in ? ws_row[bb] : 0u;
+    uint4 a[MT][kPieces];
+    uint32_t as[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u) {
+            const int p = kPieces * bb + u;
+            const bool there = in && (A4 || p < pieces);
+            a[m][u] = keep_if(there, *(const uint4*)(a_row[m] + 16 * (int64_t)(there ? p : 0)));
+        }
+        if constexpr (A4) as[m] = in ? as_row[m][bb] : 0u;
+    }
+    multiply128<A4, MT>(w, ws, a, as, acc);
+}
+
+// The steps wv, wv + waves, ... of the rows' steps, the loads of several of them (few rows of A: four) on their way at once: a wave has few steps, and
+// one after the other they are a chain of memory round trips.
 template <bool A4, int MT>
 __device__ __forceinline__ void wave_steps(const uint8_t* w_row, const uint8_t* ws_row, const char* const (&a_row)[MT],
                                            const uint8_t* const (&as_row)[MT], int Kb, int pieces, int g, int wv, int waves,
                                            f32x4_t (&acc)[MT]) {
+    constexpr int kBatch = A4 ? (MT == 4 ? 2 : 4) : (MT == 1 ? 4 : MT == 2 ? 2 : 1), kPieces = A4 ? 1 : 4;
     const int steps = (Kb + 3) / 4;
     const int whole = A4 ? Kb / 4 : pieces / 16;       // steps without an end of a row in them
     int c = wv;
-    for (; c < whole; c += waves) step128<A4, MT, false>(w_row, ws_row, a_row, as_row, 4 * c + g, Kb, pieces, acc);
-    for (; c < steps; c += waves) step128<A4, MT, true>(w_row, ws_row, a_row, as_row, 4 * c + g, Kb, pieces, acc);
+    for (; c < whole; c += kBatch * waves) {
+        uint4 w[kBatch], a[kBatch][MT][kPieces];
+        uint32_t ws[kBatch], as[kBatch][MT];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int s = c + u * waves;
+            if (u > 0 && s >= whole) break;
+            const int b = 4 * s + g;
+            w[u] = *(const uint4*)(w_row + 16 * (int64_t)b);
+            ws[u] = ws_row[b];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+#pragma unroll
+                for (int q = 0; q < kPieces; ++q) a[u][m][q] = *(const uint4*)(a_row[m] + 16 * (int64_t)(kPieces * b + q));
+                if constexpr (A4) as[u][m] = as_row[m][b];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u > 0 && c + u * waves >= whole) break;
+            multiply128<A4, MT>(w[u], ws[u], a[u], as[u], acc);
+        }
+    }
+    for (c = whole + (wv + waves - whole % waves) % waves; c < steps; c += waves)      // (the first of this wave's behind the whole ones)
+        step128<A4, MT>(w_row, ws_row, a_row, as_row, 4 * c + g, Kb, pieces, acc);
 }
 
 __device__ __forceinline__ float bias_at(const Args& a, const void* bias, int64_t n) {
@@ -108,7 +152,16 @@ __device__ __forceinline__ float bias_at(const Args& a, const void* bias, int64_
     return a.out_bf16 ? bf16_to_f32(((const uint16_t*)bias)[n]) : ((const float*)bias)[n];
 }
 
-__device__ __forceinline__ float apply(float v, int act) { return act == 2 ? v : activate(v, act); }
+// The activation; GELU of results that end in bf16 by the polynomial whose error (5e-7) is far below that rounding: the library's error function
+// took a fifth of a 4096 x 4096 x 4096 product's time.
+__device__ __forceinline__ float apply(float v, int act, bool bf16) { return act == 2 ? v : bf16 ? activate_bulk(v, act) : activate(v, act); }
+
+// sixteen bytes at any address
+__device__ __forceinline__ uint4 load_bytes(const uint8_t* p) {
+    typedef u32x4_t u32x4_byte_t __attribute__((aligned(1)));
+    const u32x4_t v = *(const u32x4_byte_t*)p;
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
 
 // four consecutive outputs n .. n + 3 of a row, those below `limit`
 __device__ __forceinline__ void store4(char* out, bool bf16, bool vec, int64_t at, int64_t n, int64_t limit, const float* v) {
@@ -133,6 +186,25 @@ __device__ __forceinline__ void store4(char* out, bool bf16, bool vec, int64_t a
     }
 }
 
+// eight, at a multiple of eight; vec: rows are whole aligned pieces of 16 bytes
+__device__ __forceinline__ void store8(char* out, bool bf16, bool vec, int64_t at, int64_t n, int64_t limit, const float* v) {
+    if (vec && n + 8 <= limit) {
+        if (bf16) {
+            *(uint4*)((uint16_t*)out + at + n) = narrow<true>(v);
+        } else {
+            *(uint4*)((float*)out + at + n) = narrow<false>(v);
+            *(uint4*)((float*)out + at + n + 4) = narrow<false>(v + 4);
+        }
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        if (n + q >= limit) break;
+        if (bf16) ((uint16_t*)out)[at + n + q] = f32_to_bf16(v[q]);
+        else ((float*)out)[at + n + q] = v[q];
+    }
+}
+
 // 16 rows of W against 16 MT rows of A per block, K shared out among its waves.
 //   kDense         rows of A as they come, rows of out too
 //   kHidden        a tile of one leaf's slots: rows of A are the slots' tokens; out is h [slot][32 blocks]
@@ -140,7 +212,7 @@ __device__ __forceinline__ void store4(char* out, bool bf16, bool vec, int64_t a
 //   kHiddenDirect  a tile is one pair: h [pair], times the pair's weight
 //   kOutputDirect  a tile is one token: the sum over its pairs as one product along k rows of h and of W
 template <bool A4, int MT, int MODE, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(const Args a) {
+__global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
     __shared__ f32x4_t part[WAVES][MT][kWave];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = lane & 15, g = lane >> 4;
     const int64_t n_blocks = (a.N + 15) / 16;
@@ -168,18 +240,15 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(const Args a) {
     const char* a_row[MT];
     const uint8_t* as_row[MT];
     if constexpr (MODE == kOutputDirect) {
-        // step c of pair i is step i * steps + c of the sum
-        const int steps = (a.Kb + 3) / 4, whole = a.pieces / 16;
-        for (int u = wv; u < a.k * steps; u += WAVES) {
-            const int i = u / steps, c = u - i * steps;
+        // step c of pair i is step i * steps + c of the sum, so that waves that pair i leaves without a step begin with pair i + 1
+        const int steps = (a.Kb + 3) / 4;
+        for (int i = 0; i < a.k; ++i) {
             const int64_t pair = first * a.k + i;
             const uint32_t e = (uint32_t)a.idx[pair];
             if (e >= a.E) continue;
-            const uint8_t* const w_row = a.w + ((int64_t)e * a.N + n) * w_row_bytes;
-            const uint8_t* const ws_row = a.w_scales + ((int64_t)e * a.N + n) * a.Kb;
             a_row[0] = a.a + pair * a.a_row;
-            if (c < whole) step128<A4, MT, false>(w_row, ws_row, a_row, as_row, 4 * c + g, a.Kb, a.pieces, acc);
-            else step128<A4, MT, true>(w_row, ws_row, a_row, as_row, 4 * c + g, a.Kb, a.pieces, acc);
+            wave_steps<A4, MT>(a.w + ((int64_t)e * a.N + n) * w_row_bytes, a.w_scales + ((int64_t)e * a.N + n) * a.Kb, a_row, as_row, a.Kb, a.pieces,
+                               g, (wv + WAVES - i * steps % WAVES) % WAVES, WAVES, acc);
         }
     } else {
         if constexpr (MODE == kHiddenDirect) {
@@ -212,13 +281,13 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(const Args a) {
         const int64_t n4 = n0 + 4 * g;
         if constexpr (MODE == kDense) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bias_at(a, a.bias, n4 + q), a.act) : 0.f;
+            for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bias_at(a, a.bias, n4 + q), a.act, a.out_bf16) : 0.f;
             store4(a.out, a.out_bf16, a.out_vec, (first + row) * a.out_row, n4, a.N, o);
         } else if constexpr (MODE == kHidden || MODE == kHiddenDirect) {
             const uint16_t* const bias = (const uint16_t*)a.bias + leaf * a.N;
             const float scale = MODE == kHiddenDirect && a.weight ? a.weight[first] : 1.0f;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bf16_to_f32(bias[n4 + q]), a.act) * scale : 0.f;
+            for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bf16_to_f32(bias[n4 + q]), a.act, true) * scale : 0.f;
             // (the row of h is whole blocks of 32: zeros behind the leaf's width)
             store4(a.out, true, true, (first + row) * a.out_row, n4, a.out_row, o);
             if (n4 + 16 >= a.N && n4 + 16 < a.out_row) {
@@ -251,58 +320,56 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(const Args a) {
 
 // ---- tiles through LDS -------------------------------------------------------------------------------------
 //
-// Many rows of A: a block of WM x WN waves takes 16 MT WM rows of A against 16 NT WN rows of W, a wave 16 MT x 16 NT results.  A stage is 128
-// elements of K (bf16 rows: 256 bytes of a row of A, 64 of W) or 256 (codes: 128 bytes of either); two stages, one on its way
-// straight to LDS while the other is multiplied.  Scale bytes go to registers, a stage ahead too.
+// Many rows of A: a block of four waves takes 16 MT rows of A against 128 rows of W, a wave all of these rows of A against 32 of W (so that codes
+// are converted once a block).  A stage is 64 elements of K (bf16 rows: 128 bytes of a row of A, 32 of W) or 128 (codes: 64 bytes of either); of the
+// three stages in LDS one is multiplied and two are on their way, straight from memory.  Two blocks share a compute unit, and one multiplies while the
+// other waits or ends.  (4096 x 4096 x 4096 and 16384 x 2048 x 768 of bf16 rows, 8192 x 4096 x 4096 of codes: 134, 59 and 117 us; a wave on 64 x 64: 145,
+// 61, 131; eight waves on 256 x 256, half of them reading while the others multiply: 138, 65, 134.)
+// The scale bytes of 128 blocks of every row (4096 elements of K) are put into LDS at once: a row's scales of one stage are a few bytes in a line of
+// their own, so that fetching them stage by stage cost as much as the codes (8192 x 4096 x 4096, four bits both: 121 us without such
+// loads, 174 with them).
 //
-// Pieces of 16 bytes in LDS are turned within their row so that the 16 lanes of a pass of an operand read (rows
+// Lane (j, g) multiplies, of a stage of bf16 rows, elements 16 g + 8 u .. + 7 in step u (pieces 2 g + u of A, four bytes of codes); of a stage of codes,
+// block g.  Pieces of 16 bytes in LDS are turned within their row so that the 16 lanes of a pass of an operand read (rows
 // {0-3, 12-15} of one g with rows {4-11} of its neighbour, then the others) meet every bank once; the turn is made by
-// the lanes' source addresses, since a load to LDS writes lane after lane:
-//   128-byte rows, pieces 2 g + u: tile_swz's; 256-byte rows, pieces 4 g + u: (row & 3) + 8 (row >> 3 & 1) further; 64-byte rows, piece g:
-//   2 (row >> 3 & 1) further.
+// the lanes' source addresses, since a load to LDS writes lane after lane: 128-byte rows as tile_swz, 64-byte rows by 2 (row >> 3 & 1), 32-byte rows
+// (read eight bytes a lane) not at all.
 __device__ const uint4 g_zero_piece = {0, 0, 0, 0};
+constexpr int kPanel = 128;      // blocks whose scales are in LDS
 
-template <int ROW> __device__ __forceinline__ int turn(int row) {
-    return ROW == 256 ? (row & 3) + 8 * ((row >> 3) & 1) : ROW == 128 ? lds_rot(row) : 2 * ((row >> 3) & 1);
-}
+template <int ROW> __device__ __forceinline__ int turn(int row) { return ROW == 128 ? lds_rot(row) : ROW == 64 ? 2 * ((row >> 3) & 1) : 0; }
 template <int ROW> __device__ __forceinline__ int lds_slot(int row, int piece) {
     constexpr int n = ROW / 16;
     return row * n + ((piece + turn<ROW>(row)) & (n - 1));
 }
+// byte of block b (of the panel) of a row: pieces of 16 exchanged so that eight rows' lie in different banks
+__device__ __forceinline__ int scale_slot(int row, int b) { return row * kPanel + (b ^ ((row & 7) << 4)); }
 
-// `count` scale bytes of a row from block b on, the first in the low byte; zeros behind the row's Kb
-template <int COUNT> __device__ __forceinline__ uint32_t load_scales(const uint8_t* row, int b, int Kb) {
-    typedef uint32_t u32_any __attribute__((aligned(1)));
-    typedef uint16_t u16_any __attribute__((aligned(1)));
-    if (b + COUNT <= Kb) return COUNT == 4 ? *(const u32_any*)(row + b) : (uint32_t) * (const u16_any*)(row + b);
-    uint32_t v = 0;
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i)
-        if (b + i < Kb) v |= (uint32_t)row[b + i] << (8 * i);
-    return v;
-}
-
-template <bool A4, int WM, int WN, int MT, int NT> struct TileShape {
-    static constexpr int kThreads = 64 * WM * WN, kWaves = WM * WN, kRows = 16 * MT * WM, kCols = 16 * NT * WN;
-    static constexpr int kARow = A4 ? 128 : 256, kWRow = A4 ? 128 : 64;         // bytes of a row in a stage
-    static constexpr int kStepBlocks = A4 ? 8 : 4;                                // blocks of 32 in a stage
+template <bool A4, int MT> struct TileShape {
+    static constexpr int kThreads = 256, kWaves = 4, NT = 2, kRows = 16 * MT, kCols = 128;
+    static constexpr int kARow = A4 ? 64 : 128, kWRow = A4 ? 64 : 32;           // bytes of a row in a stage
+    static constexpr int kStageBlocks = A4 ? 4 : 2;                               // blocks of 32 in a stage
     static constexpr int kABytes = kRows * kARow, kWBytes = kCols * kWRow, kStage = kABytes + kWBytes;
     static constexpr int kALoads = kABytes / 1024 / kWaves, kWLoads = kWBytes / 1024 / kWaves;   // a wave's loads of 1 KB a stage
     static_assert(kALoads * 1024 * kWaves == kABytes && kWLoads * 1024 * kWaves == kWBytes, "whole loads a wave");
+    static constexpr int kScaleRows = kCols + (A4 ? kRows : 0);
+    static constexpr int kLds = 3 * kStage + kScaleRows * kPanel;
 };
 
-template <bool A4, int MODE, int WM, int WN, int MT, int NT>
-__global__ __launch_bounds__(64 * WM * WN, 2) void mx4_tile_kernel(const Args a, const int64_t row_tiles, const int64_t col_tiles) {
-    typedef TileShape<A4, WM, WN, MT, NT> S;
+template <bool A4, int MODE, bool WIDE, int MT>
+__global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const int64_t row_tiles, const int64_t col_tiles) {
+    typedef TileShape<A4, MT> S;
+    constexpr int NT = S::NT;
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = lane & 15, g = lane >> 4;
-    const int wm = wv / WN, wn = wv % WN;
-    // an XCD takes a contiguous range of tiles, eight row tiles against all columns at a time
+    uint8_t* const scales = (uint8_t*)lds + 3 * S::kStage;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
+    // an XCD takes a contiguous range of tiles, kGroup row tiles against all columns at a time
+    constexpr int kGroup = 4;
     const int64_t id = xcd_contiguous_block();
     if (id >= row_tiles * col_tiles) return;
-    const int64_t group = id / (8 * col_tiles), in = id - group * 8 * col_tiles;
-    const int64_t tall = row_tiles - 8 * group < 8 ? row_tiles - 8 * group : 8;
-    const int64_t rt = 8 * group + in % tall, ct = in / tall;
+    const int64_t group = id / (kGroup * col_tiles), in = id - group * kGroup * col_tiles;
+    const int64_t tall = row_tiles - kGroup * group < kGroup ? row_tiles - kGroup * group : kGroup;
+    const int64_t rt = kGroup * group + in % tall, ct = in / tall;
     const int64_t n0 = ct * S::kCols;
     int64_t leaf = 0, first, rows;
     if constexpr (MODE == kDense) {
@@ -321,55 +388,100 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx4_tile_kernel(const Args a,
         return r;
     };
     const auto w_index = [&](int64_t n) -> int64_t { return leaf * a.N + (n0 + n < a.N ? n0 + n : a.N - 1); };
-    const int64_t w_row_bytes = (int64_t)a.Kb * 16;
 
-    // sources of this lane's pieces: piece `p` of its rows in stage 0
-    const char* a_src[S::kALoads];
-    const char* w_src[S::kWLoads];
-    int a_piece[S::kALoads], w_piece[S::kWLoads];
+    // Sources of this lane's pieces in stage 0: bytes from a base that the wave shares (from any address where WIDE says that the
+    // rows of A reach further than 32 bits).
+    const char* const a_base = uniform(MODE == kHidden ? a.a : a.a + first * a.a_row);
+    const int64_t w_row = (int64_t)a.Kb * 16;
+    const char* const w_base = uniform((const char*)a.w + (leaf * a.N + n0) * w_row);
+    typedef typename std::conditional<WIDE, int64_t, uint32_t>::type Offset;
+    Offset a_off[S::kALoads];
+    uint32_t w_off[S::kWLoads];
+    const auto a_piece = [&](int i) {
+        constexpr int n = S::kARow / 16;
+        return (lane - turn<S::kARow>((i * S::kWaves + wv) * (64 / n) + lane / n)) & (n - 1);
+    };
+    const auto w_piece = [&](int i) {
+        constexpr int n = S::kWRow / 16;
+        return (lane - turn<S::kWRow>((i * S::kWaves + wv) * (64 / n) + lane / n)) & (n - 1);
+    };
 #pragma unroll
     for (int i = 0; i < S::kALoads; ++i) {
-        constexpr int n = S::kARow / 16;
-        const int row = (i * S::kWaves + wv) * (64 / n) + lane / n;
-        a_piece[i] = (lane - turn<S::kARow>(row)) & (n - 1);
-        a_src[i] = a.a + a_index(row) * a.a_row + 16 * a_piece[i];
+        const int64_t r = a_index((i * S::kWaves + wv) * (1024 / S::kARow) + lane / (S::kARow / 16));
+        a_off[i] = (Offset)((MODE == kHidden ? r : r - first) * a.a_row + 16 * a_piece(i));
     }
 #pragma unroll
     for (int i = 0; i < S::kWLoads; ++i) {
-        constexpr int n = S::kWRow / 16;
-        const int row = (i * S::kWaves + wv) * (64 / n) + lane / n;
-        w_piece[i] = (lane - turn<S::kWRow>(row)) & (n - 1);
-        w_src[i] = (const char*)a.w + w_index(row) * w_row_bytes + 16 * w_piece[i];
+        const int64_t r = (i * S::kWaves + wv) * (1024 / S::kWRow) + lane / (S::kWRow / 16);
+        w_off[i] = (uint32_t)((n0 + r < a.N ? r : a.N - 1 - n0) * w_row + 16 * w_piece(i));
     }
-    // rows of scales of this lane's operands
-    const uint8_t* ws_row[NT];
-    const uint8_t* as_row[MT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) ws_row[n] = a.w_scales + w_index(16 * (wn * NT + n) + j) * a.Kb;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) as_row[m] = A4 ? a.a_scales + a_index(16 * (wm * MT + m) + j) * a.Kb : nullptr;
 
-    const int stages = (a.Kb + S::kStepBlocks - 1) / S::kStepBlocks;
+    const int stages = (a.Kb + S::kStageBlocks - 1) / S::kStageBlocks;
     const int a_pieces = A4 ? a.Kb : a.pieces;
-    const char* const zero = (const char*)&g_zero_piece;
-    const uint32_t lds0 = lds_address(lds);
-    uint32_t w_scale[NT], a_scale[MT];
+    const int whole = a_pieces / (S::kARow / 16) < a.Kb / S::kStageBlocks ? a_pieces / (S::kARow / 16) : a.Kb / S::kStageBlocks;
+    const uint32_t lds0 = lds_address(lds) + wv * 1024;
     const auto fetch = [&](int c, int buf) {
-        const int64_t a_off = (int64_t)c * S::kARow, w_off = (int64_t)c * S::kWRow;
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + buf * S::kStage);
+        const char* const as = a_base + (int64_t)c * S::kARow;
+        const char* const ws = w_base + (int64_t)c * S::kWRow;
+        if (c < whole) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) w_scale[n] = A4 ? load_scales<2>(ws_row[n], 8 * c + 2 * g, a.Kb) : load_scales<4>(ws_row[n], 4 * c, a.Kb);
-        if constexpr (A4) {
+            for (int i = 0; i < S::kALoads; ++i) {
+                if constexpr (WIDE) load_to_lds(as + a_off[i], at + i * S::kWaves * 1024);
+                else load_to_lds_from(as, a_off[i], at + i * S::kWaves * 1024);
+            }
 #pragma unroll
-            for (int m = 0; m < MT; ++m) a_scale[m] = load_scales<2>(as_row[m], 8 * c + 2 * g, a.Kb);
+            for (int i = 0; i < S::kWLoads; ++i) load_to_lds_from(ws, w_off[i], at + S::kABytes + i * S::kWaves * 1024);
+        } else {        // the end of the rows: zeros behind it
+            const char* const zero = (const char*)&g_zero_piece;
+#pragma unroll
+            for (int i = 0; i < S::kALoads; ++i)
+                load_to_lds(c * (S::kARow / 16) + a_piece(i) < a_pieces ? as + a_off[i] : zero, at + i * S::kWaves * 1024);
+#pragma unroll
+            for (int i = 0; i < S::kWLoads; ++i)
+                load_to_lds(c * (S::kWRow / 16) + w_piece(i) < a.Kb ? ws + w_off[i] : zero, at + S::kABytes + i * S::kWaves * 1024);
         }
-        const uint32_t at = lds0 + buf * S::kStage;
+    };
+    // Scales of blocks b0 .. b0 + 127 of all rows, zeros behind a row's end (zero codes times 2^-127): straight to LDS where rows of scales are whole
+    // aligned pieces, else through registers, BATCH loads at once (one where the accumulators are live).
+    const bool scales_aligned = a.Kb % 16 == 0 && (((uintptr_t)a.w_scales | (A4 ? (uintptr_t)a.a_scales : 0)) & 15) == 0;
+    const auto scales_of = [&](int row) { return row < S::kCols ? a.w_scales + w_index(row) * a.Kb : a.a_scales + a_index(row - S::kCols) * a.Kb; };
+    const auto fetch_scales = [&](int b0, auto BATCH) {
+        constexpr int kPieces = kPanel / 16, kAll = S::kScaleRows * kPieces, kBatch = decltype(BATCH)::value;
+        static_assert(kAll % (kBatch * S::kThreads) == 0 && kPieces == 8, "");
+        if (scales_aligned) {
+#pragma unroll 1
+            for (int i0 = 64 * wv; i0 < kAll; i0 += S::kThreads) {
+                const int i = i0 + lane, row = i / kPieces, b = b0 + 16 * ((i % kPieces) ^ (row & 7));      // (the piece that scale_slot puts here)
+                load_to_lds(b < a.Kb ? (const char*)scales_of(row) + b : (const char*)&g_zero_piece,
+                            __builtin_amdgcn_readfirstlane(lds_address(scales) + 16 * i0));
+            }
+            wait_loads<0>();
+            return;
+        }
+#pragma unroll 1
+        for (int i0 = tid; i0 < kAll; i0 += kBatch * S::kThreads) {
+            uint4 v[kBatch];
 #pragma unroll
-        for (int i = 0; i < S::kALoads; ++i)
-            load_to_lds(c * (S::kARow / 16) + a_piece[i] < a_pieces ? a_src[i] + a_off : zero, __builtin_amdgcn_readfirstlane(at + (i * S::kWaves + wv) * 1024));
+            for (int u = 0; u < kBatch; ++u) {
+                const int i = i0 + u * S::kThreads, b = b0 + 16 * (i % kPieces);
+                v[u] = load_bytes(b + 16 <= a.Kb ? scales_of(i / kPieces) + b : (const uint8_t*)&g_zero_piece);
+            }
 #pragma unroll
-        for (int i = 0; i < S::kWLoads; ++i)
-            load_to_lds(c * (S::kWRow / 16) + w_piece[i] < a.Kb ? w_src[i] + w_off : zero,
-                        __builtin_amdgcn_readfirstlane(at + S::kABytes + (i * S::kWaves + wv) * 1024));
+            for (int u = 0; u < kBatch; ++u) {
+                const int i = i0 + u * S::kThreads, b = b0 + 16 * (i % kPieces);
+                if (b < a.Kb && b + 16 > a.Kb) {
+                    const uint8_t* const src = scales_of(i / kPieces) + b;
+                    uint32_t q[4] = {0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (b + e < a.Kb) q[e / 4] |= (uint32_t)src[e] << (8 * (e % 4));
+                    v[u] = make_uint4(q[0], q[1], q[2], q[3]);
+                }
+                *(uint4*)(scales + scale_slot(i / kPieces, 16 * (i % kPieces))) = v[u];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
 
     f32x4_t acc[NT][MT];
@@ -378,147 +490,372 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx4_tile_kernel(const Args a,
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-    fetch(0, 0);
-    for (int c = 0; c < stages; ++c) {
-        // the stage is there (this wave's part, then everybody's), and nobody reads the other buffer any more
-        wait_loads<0>();
-        uint32_t ws[NT], as[MT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) ws[n] = w_scale[n];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(ws[n]));      // (the compiler waits for its loads here, not behind the next stage's)
-        if constexpr (A4) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m) as[m] = a_scale[m];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) asm volatile("" : "+v"(as[m]));
-        }
-        __syncthreads();
-        if (c + 1 < stages) fetch(c + 1, (c + 1) & 1);
-        const uint4* const la = (const uint4*)(lds + (c & 1) * S::kStage);
-        const uint4* const lw = (const uint4*)(lds + (c & 1) * S::kStage + S::kABytes);
-        if constexpr (A4) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint4 fa[MT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) fa[m] = la[lds_slot<128>(16 * (wm * MT + m) + j, 2 * g + u)];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint4 fw = lw[lds_slot<128>(16 * (wn * NT + n) + j, 2 * g + u)];
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[n][m] = mfma4(fw, u ? ws[n] >> 8 : ws[n], fa[m], u ? as[m] >> 8 : as[m], acc[n][m]);
-                }
-            }
-        } else {
-            uint4 fw[NT];
-            float s[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                fw[n] = lw[lds_slot<64>(16 * (wn * NT + n) + j, g)];
-                s[n] = __uint_as_float(((ws[n] >> (8 * g)) & 255u) << 23);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                bf16x8_t fa[MT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) fa[m] = __builtin_bit_cast(bf16x8_t, la[lds_slot<256>(16 * (wm * MT + m) + j, 4 * g + u)]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const bf16x8_t f = dequantise8(u == 0 ? fw[n].x : u == 1 ? fw[n].y : u == 2 ? fw[n].z : fw[n].w, s[n]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, fa[m], acc[n][m], 0, 0, 0);
-                }
-            }
-        }
-    }
-
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int64_t row = 16 * (wm * MT + m) + j;
-        if (row >= rows) continue;
-        int64_t to = first + row;
-        float scale = 1.0f;
-        if constexpr (MODE == kOutput) {
-            to = a.perm[to];
-            if (a.k == 1 && a.weight) scale = a.weight[to];
-        }
+    constexpr int kLoads = S::kALoads + S::kWLoads, kSteps = A4 ? 1 : 2;
+    uint4 fa[kSteps][MT], fw[NT];        // (bf16 rows: fw[.].xy are the codes of both steps of a stage)
+    uint32_t as[MT], ws[NT];
+    const auto read = [&](int c, int buf) {
+        const uint4* const la = (const uint4*)(lds + buf * S::kStage);
+        const char* const lw = lds + buf * S::kStage + S::kABytes;
+        const int b0 = c * S::kStageBlocks % kPanel, b = b0 + (A4 ? g : g >> 1);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int64_t n4 = n0 + 16 * (wn * NT + n) + 4 * g;
-            const int64_t limit = MODE == kHidden ? a.out_row : a.N;
-            if (n4 >= limit) continue;
-            float o[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float v = acc[n][m][q];
-                if constexpr (MODE == kDense) o[q] = n4 + q < a.N ? apply(v + bias_at(a, a.bias, n4 + q), a.act) : 0.f;
-                else if constexpr (MODE == kHidden) o[q] = n4 + q < a.N ? apply(v + bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n4 + q]), a.act) : 0.f;
-                else o[q] = n4 + q < a.N ? (v + bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n4 + q])) * scale : 0.f;
+            const int row = 16 * (wv * NT + n) + j;
+            if constexpr (A4) {
+                fw[n] = ((const uint4*)lw)[lds_slot<64>(row, g)];
+            } else {
+                const uint2 v = *(const uint2*)(lw + row * 32 + 8 * g);
+                fw[n].x = v.x;
+                fw[n].y = v.y;
             }
-            store4(a.out, MODE == kHidden || a.out_bf16, MODE == kHidden || a.out_vec, to * a.out_row, n4, limit, o);
+            ws[n] = scales[scale_slot(row, b)];
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int row = 16 * m + j;
+#pragma unroll
+            for (int u = 0; u < kSteps; ++u) fa[u][m] = la[A4 ? lds_slot<64>(row, g) : lds_slot<128>(row, 2 * g + u)];
+            if constexpr (A4) as[m] = scales[scale_slot(S::kCols + row, b0 + g)];
+        }
+    };
+    const auto multiply = [&]() {
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (A4) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[n][m] = mfma4(fw[n], ws[n], fa[0][m], as[m], acc[n][m]);
+                } else {
+                    const bf16x8_t f = dequantise8(u == 0 ? fw[n].x : fw[n].y, __uint_as_float(ws[n] << 23));
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+                        acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, __builtin_bit_cast(bf16x8_t, fa[u][m]), acc[n][m], 0, 0, 0);
+                }
+            }
+    };
+    const auto barrier = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    fetch(0, 0);
+    if (stages > 1) fetch(1, 1);
+    if (stages > 2) fetch(2, 2);
+    fetch_scales(0, std::integral_constant<int, 2>());
+    wait_loads<0>();
+    __syncthreads();
+    int buf = 0;
+    // Everybody has read stage c: its buffer takes stage c + 3, and at the end of a panel of scales the next one comes.
+    const auto turn_over = [&](int c) {
+        if (c + 3 < stages) fetch(c + 3, buf);
+        if ((c + 1) * S::kStageBlocks % kPanel == 0 && c + 1 < stages) {
+            fetch_scales((c + 1) * S::kStageBlocks, std::integral_constant<int, 1>());
+            barrier();
+        }
+    };
+    for (int c = 0; c < stages; ++c) {
+        read(c, buf);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (c + 2 < stages) wait_loads<kLoads>();      // this wave's part of stage c + 1 is there
+        else wait_loads<0>();
+        barrier();
+        turn_over(c);
+        multiply();
+        buf = buf == 2 ? 0 : buf + 1;
+    }
+
+    // Results through LDS, half of the wave's rows at a time, so that they leave as whole rows of 16 NT columns, eight a lane, from a loop:
+    // written out for every accumulator the epilogue was more code than the instruction cache takes, and fetching it took longer than
+    // the stages of a short K.
+    constexpr int kHalf = MT / 2, kPitch = 16 * NT + 4, kLanes = 2 * NT, kRowsAtOnce = 64 / kLanes;
+    static_assert(S::kWaves * 16 * kHalf * kPitch * 4 <= S::kLds, "results fit where the stages were");
+    float* const part = (float*)lds + wv * 16 * kHalf * kPitch;
+    const int64_t limit = MODE == kHidden ? a.out_row : a.N;
+    const int64_t n8 = n0 + 16 * NT * wv + 8 * (lane % kLanes);
+    float bias[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        bias[q] = n8 + q >= a.N ? 0.f : MODE == kDense ? bias_at(a, a.bias, n8 + q) : bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n8 + q]);
+    __syncthreads();
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int m = 0; m < kHalf; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) *(f32x4_t*)(part + (16 * m + j) * kPitch + 16 * n + 4 * g) = half == 0 ? acc[n][m] : acc[n][m + kHalf];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int64_t row0 = 16 * half * kHalf;
+#pragma unroll 1
+        for (int r = lane / kLanes; r < 16 * kHalf; r += kRowsAtOnce) {
+            if (row0 + r >= rows || n8 >= limit) continue;
+            int64_t to = first + row0 + r;
+            float scale = 1.0f;
+            if constexpr (MODE == kOutput) {
+                to = a.perm[to];
+                if (a.k == 1 && a.weight) scale = a.weight[to];
+            }
+            const float* const v = part + r * kPitch + 8 * (lane % kLanes);
+            float o[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                o[q] = v[q] + bias[q];
+                if constexpr (MODE == kOutput) o[q] *= scale;
+                else o[q] = apply(o[q], a.act, MODE == kHidden || a.out_bf16);
+                if constexpr (MODE == kHidden) o[q] = n8 + q < a.N ? o[q] : 0.f;
+            }
+            store8(a.out, MODE == kHidden || a.out_bf16, MODE == kHidden || a.out_vec, to * a.out_row, n8, limit, o);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+template <bool A4, int MODE, int MT> hipError_t launch_tiles(Args a, int64_t row_tiles, hipStream_t s) {
+    typedef TileShape<A4, MT> S;
+    const int64_t col_tiles = ((MODE == kHidden ? a.out_row : a.N) + S::kCols - 1) / S::kCols;
+    const int64_t blocks = (row_tiles * col_tiles + kXcds - 1) / kXcds * kXcds;
+    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    a.out_vec = a.out_row % (a.out_bf16 ? 8 : 4) == 0 && ((uintptr_t)a.out & 15) == 0;
+    // rows of A within 32 bits of the first that a block reaches: its own always (K <= 2^22), any token's not always
+    const bool wide = MODE == kHidden && a.T * a.a_row >= (int64_t)1 << 32;
+    note_launch("mx4_tile_kernel<%s,%d,%s>", A4 ? "mx4" : "bf16", S::kRows, MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : "output");
+    const auto kernel = wide ? mx4_tile_kernel<A4, MODE, MODE == kHidden, MT> : mx4_tile_kernel<A4, MODE, false, MT>;
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+    if (e != hipSuccess) return e;
+    kernel<<<dim3((unsigned)blocks), S::kThreads, S::kLds, s>>>(a, row_tiles, col_tiles);
+    return hipGetLastError();
+}
+
+// Rows of A a tile: 128 once there are enough such tiles for two a compute unit, else 64 (512 x 4096 x 4096 of bf16 rows, 128 or 256 tiles: 46 or
+// 33 us; 16384 x 2048 x 768, 768 or 1536 tiles: 59 or 63).
+int tile_rows_for(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128) >= 2 * device_info().cus ? 128 : 64; }
+
+template <bool A4, int MODE> hipError_t launch_tiles(const Args& a, int64_t row_tiles, int tile_rows, hipStream_t s) {
+    return tile_rows == 128 ? launch_tiles<A4, MODE, 8>(a, row_tiles, s) : launch_tiles<A4, MODE, 4>(a, row_tiles, s);
+}
+
+// ---- a block a token ---------------------------------------------------------------------------------------
+//
+// Narrow leaves: one launch, no scratch.  All hidden activations of the token's k leaves (a wave's share of D, four tiles of 16 neurons at a
+// time, the waves' sums met in LDS), then all its outputs (a wave's tiles of 16, the whole sum over the pairs).  Bound by the latency of the two
+// dependent reads of weights.
+constexpr int kTokenWaves = 8, kTokenTiles = 4;
+
+// Steps c0, c0 + stride, ... of one row of A (in global memory or LDS) against up to kTokenTiles tiles of 16 rows of W.
+__device__ __forceinline__ void tiles_steps(const uint8_t* const (&w_row)[kTokenTiles], const uint8_t* const (&ws_row)[kTokenTiles], int tiles,
+                                            const char* a_row, int Kb, int pieces, int g, int c0, int stride, f32x4_t (&acc)[kTokenTiles]) {
+    const int steps = (Kb + 3) / 4;
+    for (int c = c0; c < steps; c += stride) {
+        const int b = 4 * c + g;
+        const bool in = b < Kb;
+        const int bb = in ? b : Kb - 1;
+        uint4 w[kTokenTiles], x[4];
+        uint32_t ws[kTokenTiles];
+#pragma unroll
+        for (int t = 0; t < kTokenTiles; ++t) {
+            if (t >= tiles) break;
+            w[t] = *(const uint4*)(w_row[t] + 16 * (int64_t)bb);
+            ws[t] = ws_row[t][bb];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const bool there = in && 4 * bb + u < pieces;
+            x[u] = keep_if(there, *(const uint4*)(a_row + 16 * (int64_t)(there ? 4 * bb + u : 0)));
+        }
+#pragma unroll
+        for (int t = 0; t < kTokenTiles; ++t) {
+            if (t >= tiles) break;
+            const uint4 v = keep_if(in, w[t]);
+            const float s = __uint_as_float((in ? ws[t] : 0u) << 23);
+            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequantise8(q[u], s), __builtin_bit_cast(bf16x8_t, x[u]), acc[t], 0, 0, 0);
         }
     }
 }
 
-template <bool A4, int MODE, int WM, int WN, int MT, int NT> hipError_t launch_tiles(const Args& a, int64_t row_tiles, hipStream_t s) {
-    typedef TileShape<A4, WM, WN, MT, NT> S;
-    const int64_t width = MODE == kHidden ? a.out_row : a.N;
-    const int64_t col_tiles = (width + S::kCols - 1) / S::kCols;
-    const int64_t blocks = (row_tiles * col_tiles + kXcds - 1) / kXcds * kXcds;
-    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
-    note_launch("mx4_tile_kernel<%s,%d,%d,%s>", A4 ? "mx4" : "bf16", S::kRows, S::kCols, MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : "output");
-    const auto kernel = mx4_tile_kernel<A4, MODE, WM, WN, MT, NT>;
-    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * S::kStage);
-    if (e != hipSuccess) return e;
-    kernel<<<dim3((unsigned)blocks), S::kThreads, 2 * S::kStage, s>>>(a, row_tiles, col_tiles);
-    return hipGetLastError();
+__global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args a, const Args b) {
+    extern __shared__ __align__(16) uint16_t h[];          // [k][h_row]
+    __shared__ float part[2][kTokenWaves][16 * kTokenTiles];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = lane & 15, g = lane >> 4;
+    const int64_t t = blockIdx.x;
+    const int h_row = (int)a.out_row, h_tiles = h_row / 16;
+    int round = 0;
+    for (int i = 0; i < a.k; ++i) {
+        const uint32_t e = (uint32_t)a.idx[t * a.k + i];
+        if (e >= a.E) continue;                            // (not read below)
+        const float scale = a.weight ? a.weight[t * a.k + i] : 1.0f;
+        for (int t0 = 0; t0 < h_tiles; t0 += kTokenTiles, round ^= 1) {
+            const uint8_t *w_row[kTokenTiles], *ws_row[kTokenTiles];
+            f32x4_t acc[kTokenTiles];
+#pragma unroll
+            for (int u = 0; u < kTokenTiles; ++u) {
+                const int64_t n = 16 * (t0 + u) + j, r = (int64_t)e * a.N + (n < a.N ? n : a.N - 1);
+                w_row[u] = a.w + r * a.Kb * 16;
+                ws_row[u] = a.w_scales + r * a.Kb;
+                acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+            tiles_steps(w_row, ws_row, h_tiles - t0 < kTokenTiles ? h_tiles - t0 : kTokenTiles, a.a + t * a.a_row, a.Kb, a.pieces, g, wv, kTokenWaves, acc);
+            if (j == 0) {
+#pragma unroll
+                for (int u = 0; u < kTokenTiles; ++u) *(f32x4_t*)&part[round][wv][16 * u + 4 * g] = acc[u];
+            }
+            __syncthreads();
+            const int n = 16 * t0 + tid;
+            if (tid < 16 * kTokenTiles && n < h_row) {
+                float v = part[round][0][tid];
+#pragma unroll
+                for (int w = 1; w < kTokenWaves; ++w) v += part[round][w][tid];
+                v = n < a.N ? apply(v + bf16_to_f32(((const uint16_t*)a.bias)[(int64_t)e * a.N + n]), a.act, true) * scale : 0.f;
+                h[i * h_row + n] = f32_to_bf16(v);
+            }
+        }
+    }
+    __syncthreads();
+    const int64_t o_tiles = (b.N + 15) / 16;
+    for (int64_t t0 = (int64_t)wv * kTokenTiles; t0 < o_tiles; t0 += kTokenWaves * kTokenTiles) {
+        const int tiles = o_tiles - t0 < kTokenTiles ? (int)(o_tiles - t0) : kTokenTiles;
+        f32x4_t acc[kTokenTiles];
+        float bias[kTokenTiles][4];
+#pragma unroll
+        for (int u = 0; u < kTokenTiles; ++u) {
+            acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) bias[u][q] = 0.f;
+        }
+        for (int i = 0; i < b.k; ++i) {
+            const uint32_t e = (uint32_t)b.idx[t * b.k + i];
+            if (e >= b.E) continue;
+            const float scale = b.weight ? b.weight[t * b.k + i] : 1.0f;
+            const uint8_t *w_row[kTokenTiles], *ws_row[kTokenTiles];
+#pragma unroll
+            for (int u = 0; u < kTokenTiles; ++u) {
+                const int64_t n = 16 * (t0 + u) + j, r = (int64_t)e * b.N + (n < b.N ? n : b.N - 1);
+                w_row[u] = b.w + r * b.Kb * 16;
+                ws_row[u] = b.w_scales + r * b.Kb;
+            }
+            tiles_steps(w_row, ws_row, tiles, (const char*)(h + i * h_row), b.Kb, b.pieces, g, 0, 1, acc);
+            if (j == 0) {
+#pragma unroll
+                for (int u = 0; u < kTokenTiles; ++u)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int64_t n = 16 * (t0 + u) + 4 * g + q;
+                        if (n < b.N) bias[u][q] = fmaf(scale, bf16_to_f32(((const uint16_t*)b.bias)[(int64_t)e * b.N + n]), bias[u][q]);
+                    }
+            }
+        }
+        if (j == 0) {
+#pragma unroll
+            for (int u = 0; u < kTokenTiles; ++u) {
+                float o[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) o[q] = acc[u][q] + bias[u][q];
+                store4(b.out, true, b.out_vec, t * b.out_row, 16 * (t0 + u) + 4 * g, b.N, o);
+            }
+        }
+    }
 }
 
 // ---- grouping of the pairs by leaf -------------------------------------------------------------------------
 //
 // rank[p] = place of pair p among its leaf's; which pair gets which place depends on the order of the atomics, and
 // nothing else does: a row's sums do not know its place in a tile.
-__global__ __launch_bounds__(256) void group_count_kernel(const int32_t* __restrict__ idx, int64_t P, int64_t E, int32_t* __restrict__ count,
+constexpr int kGroupPairs = 1024;         // pairs of a block of group_count_kernel
+constexpr int kGroupLdsLeaves = 8192;     // leaves whose counts fit LDS
+
+// Counts of a block's pairs meet in LDS first (LDS: E <= kGroupLdsLeaves): 16384 pairs on 16 leaves, all by atomics on memory, took 46 us.
+template <bool LDS>
+__global__ __launch_bounds__(256) void group_count_kernel(const int32_t* __restrict__ idx, int64_t P, int E, int32_t* __restrict__ count,
                                                           int32_t* __restrict__ rank) {
-    const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (p >= P) return;
-    const uint32_t e = (uint32_t)idx[p];
-    if (e < E) rank[p] = atomicAdd(count + e, 1);
+    extern __shared__ int32_t own[];
+    const int64_t p0 = (int64_t)blockIdx.x * kGroupPairs + threadIdx.x;
+    if (!LDS) {
+#pragma unroll
+        for (int i = 0; i < kGroupPairs / 256; ++i) {
+            const int64_t p = p0 + 256 * i;
+            const uint32_t e = p < P ? (uint32_t)idx[p] : ~0u;
+            if (e < (uint32_t)E) rank[p] = atomicAdd(count + e, 1);
+        }
+        return;
+    }
+    for (int e = threadIdx.x; e < E; e += 256) own[e] = 0;
+    __syncthreads();
+    uint32_t e[kGroupPairs / 256];
+    int32_t r[kGroupPairs / 256];
+#pragma unroll
+    for (int i = 0; i < kGroupPairs / 256; ++i) {
+        e[i] = p0 + 256 * i < P ? (uint32_t)idx[p0 + 256 * i] : ~0u;
+        if (e[i] < (uint32_t)E) r[i] = atomicAdd(own + e[i], 1);
+    }
+    __syncthreads();
+    for (int l = threadIdx.x; l < E; l += 256)
+        if (own[l]) own[l] = atomicAdd(count + l, own[l]);      // from here on the places before the block's
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kGroupPairs / 256; ++i)
+        if (e[i] < (uint32_t)E) rank[p0 + 256 * i] = own[e[i]] + r[i];
+}
+
+// exclusive sums over a block of 1024 threads
+__device__ __forceinline__ void block_scan(int32_t& x, int32_t& y, int32_t (&sums)[2][16]) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int32_t x0 = x, y0 = y;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t u = __shfl_up(x, d, 64), v = __shfl_up(y, d, 64);
+        x += lane >= d ? u : 0;
+        y += lane >= d ? v : 0;
+    }
+    if (lane == 63) {
+        sums[0][wv] = x;
+        sums[1][wv] = y;
+    }
+    __syncthreads();
+    x -= x0;
+    y -= y0;
+    for (int w = 0; w < wv; ++w) {
+        x += sums[0][w];
+        y += sums[1][w];
+    }
 }
 
 // start[E + 1], tile_start[E + 1]: exclusive sums of the counts and of the tiles of `tile_rows` slots
-__global__ __launch_bounds__(1024) void group_scan_kernel(const int32_t* __restrict__ count, int64_t E, int tile_rows, int32_t* __restrict__ start,
-                                                          int32_t* __restrict__ tile_start) {
-    __shared__ int32_t sum[2][1024];
+__device__ __forceinline__ void scan_leaves(const int32_t* count, int64_t E, int tile_rows, int32_t* start, int32_t* tile_start, int32_t (&sums)[2][16]) {
     const int tid = threadIdx.x;
-    const int64_t per = (E + 1023) / 1024, e0 = tid * per, e1 = e0 + per < E ? e0 + per : E;
+    const int64_t per = (E + 1023) / 1024, e0 = tid * per < E ? tid * per : E, e1 = e0 + per < E ? e0 + per : E;
     int32_t c = 0, t = 0;
     for (int64_t e = e0; e < e1; ++e) {
         c += count[e];
         t += (count[e] + tile_rows - 1) / tile_rows;
     }
-    sum[0][tid] = c;
-    sum[1][tid] = t;
-    __syncthreads();
-    for (int d = 1; d < 1024; d <<= 1) {
-        const int32_t v0 = tid >= d ? sum[0][tid - d] : 0, v1 = tid >= d ? sum[1][tid - d] : 0;
-        __syncthreads();
-        sum[0][tid] += v0;
-        sum[1][tid] += v1;
-        __syncthreads();
-    }
-    c = sum[0][tid] - c;
-    t = sum[1][tid] - t;
+    block_scan(c, t, sums);
     for (int64_t e = e0; e < e1; ++e) {
+        const int32_t n = count[e];
         start[e] = c;
         tile_start[e] = t;
-        c += count[e];
-        t += (count[e] + tile_rows - 1) / tile_rows;
+        c += n;
+        t += (n + tile_rows - 1) / tile_rows;
     }
-    if (tid == 1023) {
-        start[E] = sum[0][1023];
-        tile_start[E] = sum[1][1023];
+    if (e0 < E && e1 == E) {
+        start[E] = c;
+        tile_start[E] = t;
+    }
+}
+
+__global__ __launch_bounds__(1024) void group_scan_kernel(const int32_t* __restrict__ count, int64_t E, int tile_rows, int32_t* __restrict__ start,
+                                                          int32_t* __restrict__ tile_start) {
+    __shared__ int32_t sums[2][16];
+    scan_leaves(count, E, tile_rows, start, tile_start, sums);
+}
+
+__device__ __forceinline__ void place(int64_t p, uint32_t e, int32_t r, int tile_rows, const int32_t* start, const int32_t* tile_start,
+                                      int32_t* __restrict__ perm, int32_t* __restrict__ tile_leaf, int32_t* __restrict__ tile_slot) {
+    const int32_t slot = start[e] + r;
+    perm[slot] = (int32_t)p;
+    if (r % tile_rows == 0) {
+        const int32_t tile = tile_start[e] + r / tile_rows;
+        tile_leaf[tile] = (int32_t)e;
+        tile_slot[tile] = slot;
     }
 }
 
@@ -529,13 +866,35 @@ __global__ __launch_bounds__(256) void group_place_kernel(const int32_t* __restr
     const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (p >= P) return;
     const uint32_t e = (uint32_t)idx[p];
-    if (e >= E) return;
-    const int32_t r = rank[p], slot = start[e] + r;
-    perm[slot] = (int32_t)p;
-    if (r % tile_rows == 0) {
-        const int32_t tile = tile_start[e] + r / tile_rows;
-        tile_leaf[tile] = (int32_t)e;
-        tile_slot[tile] = slot;
+    if (e < E) place(p, e, rank[p], tile_rows, start, tile_start, perm, tile_leaf, tile_slot);
+}
+
+// All of it in one block, for few pairs: counts, sums and places in LDS (a second pass of atomics gives the places).
+constexpr int64_t kGroupOnePairs = 32768, kGroupOneLeaves = 4096;
+__global__ __launch_bounds__(1024) void group_one_kernel(const int32_t* __restrict__ idx, int P, int E, int tile_rows, int32_t* __restrict__ start,
+                                                         int32_t* __restrict__ tile_start, int32_t* __restrict__ perm, int32_t* __restrict__ tile_leaf,
+                                                         int32_t* __restrict__ tile_slot) {
+    extern __shared__ int32_t counts[];      // counts [E], start [E + 1], tile_start [E + 1]
+    __shared__ int32_t sums[2][16];
+    int32_t *const lds_start = counts + E, *const lds_tiles = lds_start + E + 1;
+    for (int e = threadIdx.x; e < E; e += 1024) counts[e] = 0;
+    __syncthreads();
+    for (int p = threadIdx.x; p < P; p += 1024) {
+        const uint32_t e = (uint32_t)idx[p];
+        if (e < (uint32_t)E) atomicAdd(counts + e, 1);
+    }
+    __syncthreads();
+    scan_leaves(counts, E, tile_rows, lds_start, lds_tiles, sums);
+    __syncthreads();
+    for (int e = threadIdx.x; e <= E; e += 1024) {
+        start[e] = lds_start[e];
+        tile_start[e] = lds_tiles[e];
+        if (e < E) counts[e] = 0;
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < P; p += 1024) {
+        const uint32_t e = (uint32_t)idx[p];
+        if (e < (uint32_t)E) place(p, e, atomicAdd(counts + e, 1), tile_rows, lds_start, lds_tiles, perm, tile_leaf, tile_slot);
     }
 }
 
@@ -623,8 +982,9 @@ hipError_t launch_mx4_product(const Mx4Product& p, hipStream_t s) {
     a.out_bf16 = p.out_bf16;
     a.out_vec = p.N % 4 == 0 && ((uintptr_t)p.out & (p.out_bf16 ? 7 : 15)) == 0;
     if (p.T >= 128) {
-        if (a4) return launch_tiles<true, kDense, 2, 4, 4, 4>(a, (p.T + 127) / 128, s);
-        return launch_tiles<false, kDense, 2, 4, 4, 4>(a, (p.T + 127) / 128, s);
+        const int tile_rows = tile_rows_for(p.T, p.N);
+        const int64_t tiles = (p.T + tile_rows - 1) / tile_rows;
+        return a4 ? launch_tiles<true, kDense>(a, tiles, tile_rows, s) : launch_tiles<false, kDense>(a, tiles, tile_rows, s);
     }
     const int mt = rows_tile(p.T);
     const int64_t tiles = (p.T + 16 * mt - 1) / (16 * mt);
@@ -671,22 +1031,35 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     b.pieces = (int)(h_row / 8);
     b.out_vec = p.O % 4 == 0 && ((uintptr_t)p.out & 7) == 0;
     hipError_t e;
+    // Few pairs, or few of them a leaf: grouping gains nothing.  Leaves of few bytes go a block a token (one launch); others are spread over the chip.
+    const int64_t leaf_bytes = (int64_t)p.L * 16 * a.Kb + p.O * 16 * b.Kb, h_bytes = 2 * h_row * p.k;
+    if ((P <= 32 || P <= 4 * p.E) && p.k * leaf_bytes <= 256 * 1024 && h_bytes <= 32 * 1024) {
+        note_launch("mx4_token_kernel");
+        mx4_token_kernel<<<dim3((unsigned)p.T), 64 * kTokenWaves, (size_t)h_bytes, s>>>(a, b);
+        return hipGetLastError();
+    }
     if (P <= 32) {
         if ((e = launch_rows<false, kHiddenDirect>(a, P, 1, s)) != hipSuccess) return e;
         return launch_rows<false, kOutputDirect>(b, p.T, 1, s);
     }
     const bool large = P / p.E >= 64;
     const int mt = rows_tile(P / p.E);
-    const int tile_rows = large ? 128 : 16 * mt;
+    const int tile_rows = large ? tile_rows_for(P, p.L < p.O ? p.L : p.O) : 16 * mt;
     const int64_t tiles = P / tile_rows + (p.E < P ? p.E : P);
     int32_t *const count = words(at.count), *const start = words(at.start), *const tile_start = words(at.tile_start);
     int32_t *const rank = words(at.rank), *const perm = words(at.perm), *const tile_leaf = words(at.tile_leaf), *const tile_slot = words(at.tile_slot);
-    if ((e = launch_zero(count, (p.E + 3) / 4 * 4, s)) != hipSuccess) return e;   // (whole pieces: the region is of 256 bytes)
-    const dim3 pairs((unsigned)((P + 255) / 256));
-    note_launch("group_kernels");
-    group_count_kernel<<<pairs, 256, 0, s>>>(p.idx, P, p.E, count, rank);
-    group_scan_kernel<<<1, 1024, 0, s>>>(count, p.E, tile_rows, start, tile_start);
-    group_place_kernel<<<pairs, 256, 0, s>>>(p.idx, P, p.E, tile_rows, rank, start, tile_start, perm, tile_leaf, tile_slot);
+    if (P <= kGroupOnePairs && p.E <= kGroupOneLeaves) {
+        note_launch("group_one_kernel");
+        group_one_kernel<<<1, 1024, (size_t)(3 * p.E + 2) * 4, s>>>(p.idx, (int)P, (int)p.E, tile_rows, start, tile_start, perm, tile_leaf, tile_slot);
+    } else {
+        if ((e = launch_zero(count, (p.E + 3) / 4 * 4, s)) != hipSuccess) return e;   // (whole pieces: the region is of 256 bytes)
+        note_launch("group kernels");
+        const dim3 blocks((unsigned)((P + kGroupPairs - 1) / kGroupPairs));
+        if (p.E <= kGroupLdsLeaves) group_count_kernel<true><<<blocks, 256, (size_t)p.E * 4, s>>>(p.idx, P, (int)p.E, count, rank);
+        else group_count_kernel<false><<<blocks, 256, 0, s>>>(p.idx, P, (int)p.E, count, rank);
+        group_scan_kernel<<<1, 1024, 0, s>>>(count, p.E, tile_rows, start, tile_start);
+        group_place_kernel<<<dim3((unsigned)((P + 255) / 256)), 256, 0, s>>>(p.idx, P, p.E, tile_rows, rank, start, tile_start, perm, tile_leaf, tile_slot);
+    }
     if ((e = hipGetLastError()) != hipSuccess) return e;
     a.perm = b.perm = perm;
     a.tile_leaf = b.tile_leaf = tile_leaf;
@@ -700,8 +1073,8 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
         b.out_vec = p.O % 4 == 0;
     }
     if (large) {
-        if ((e = launch_tiles<false, kHidden, 2, 4, 4, 4>(a, tiles, s)) != hipSuccess) return e;
-        if ((e = launch_tiles<false, kOutput, 2, 4, 4, 4>(b, tiles, s)) != hipSuccess) return e;
+        if ((e = launch_tiles<false, kHidden>(a, tiles, tile_rows, s)) != hipSuccess) return e;
+        if ((e = launch_tiles<false, kOutput>(b, tiles, tile_rows, s)) != hipSuccess) return e;
     } else {
         if ((e = launch_rows<false, kHidden>(a, tiles, mt, s)) != hipSuccess) return e;
         if ((e = launch_rows<false, kOutput>(b, tiles, mt, s)) != hipSuccess) return e;

@@ -70,17 +70,15 @@ def leaves(x, w1, b1, w2, b2, idx, weight, name):
     scaled before it), then a sum over width, the mixture over k in single precision, half a step of bf16."""
     T, O = x.shape[0], w2.shape[1]
     y, tol = np.zeros((T, O)), np.zeros((T, O))
-    for t in range(T):
-        for i in range(idx.shape[1]):
-            e = idx[t, i]
-            if e < 0 or e >= len(w1):
-                continue
-            h, he = product(x[t:t + 1], w1[e], b1[e], name, "bf16")
-            g = 1.0 if weight is None else weight[t, i]
-            v = h[0] @ w2[e].T + b2[e]
-            size = np.abs(h[0]) @ np.abs(w2[e]).T + np.abs(b2[e])
-            y[t] += g * v
-            tol[t] += abs(g) * ((he[0] + 2.0 ** -23 * np.abs(h[0])) @ np.abs(w2[e]).T + (w2.shape[2] * idx.shape[1] + 4) * 2.0 ** -23 * size)
+    for e in np.unique(idx):
+        if e < 0 or e >= len(w1):
+            continue
+        t, i = np.nonzero(idx == e)
+        h, he = product(x[t], w1[e], b1[e], name, "bf16")
+        g = np.ones((len(t), 1)) if weight is None else weight[t, i][:, None]
+        size = np.abs(h) @ np.abs(w2[e]).T + np.abs(b2[e])
+        np.add.at(y, t, g * (h @ w2[e].T + b2[e]))
+        np.add.at(tol, t, np.abs(g) * ((he + 2.0 ** -23 * np.abs(h)) @ np.abs(w2[e]).T + (w2.shape[2] * idx.shape[1] + 4) * 2.0 ** -23 * size))
     return y, tol + HALF["bf16"] * (np.abs(y) + tol) + 2.0 ** -126
 
 

@@ -122,7 +122,7 @@ def _matrix(rng, shape, scale):
     return c, s, R.values(c, s, shape[-1])
 
 
-SIZES = [(1, 32, 16), (1, 4096, 256), (3, 31, 5), (16, 128, 64), (17, 100, 33), (31, 160, 48), (33, 1000, 77), (64, 96, 130), (65, 257, 31),
+SIZES = [(1, 32, 16), (1, 8192, 64), (130, 4160, 140), (150, 8230, 40), (3000, 264, 3200), (2050, 100, 4100), (1, 4096, 256), (3, 31, 5), (16, 128, 64), (17, 100, 33), (31, 160, 48), (33, 1000, 77), (64, 96, 130), (65, 257, 31),
          (129, 512, 257), (200, 777, 129), (257, 2048, 96), (300, 64, 515), (513, 320, 256)]
 
 
@@ -214,6 +214,21 @@ LEAVES = [
     (300, 2, 2,  128, 264, 100, True),
     (260, 1, 1,  72,  136, 129, False),
     (400, 8, 8,  40,  24,  48,  True),
+    # few pairs with leaves too large for a block a token
+    (1,   1, 2,  1024, 520, 600, True),
+    (3,   2, 4,  1096, 521, 601, True),
+    (5,   6, 9,  2000, 264, 333, False),
+    (2,   3, 3,  333, 4100, 128, True),
+    # grouped: tiles of 16, 32 and 64 rows, and of 64 and 128 through LDS
+    (60,  1, 4,  520, 1024, 700, True),
+    (40,  2, 3,  96,  40,  36,  True),
+    (150, 1, 3,  160, 130, 257, True),
+    (700, 2, 5,  296, 136, 300, True),
+    (4100, 8, 2, 136, 1032, 1100, True),
+    # more pairs, or leaves, than one block groups
+    (4200, 8, 8, 40,  24,  16,  True),
+    (5001, 8, 4100, 32, 16, 8,  True),
+    (4700, 8, 9000, 32, 16, 8,  True),
 ]
 
 
