@@ -5,7 +5,7 @@ behind them; this layer can, so it checks every tensor's shape and dtype against
 Definition's sizes (2^depth - 1 node rows, 2^depth leaves of leaf_width neurons, D inputs,
 O outputs) on the host, before any pointer reaches the library.
 
-The four forward entry points go through a native module first (csrc/fff_torch.cpp), which makes
+The forward entry points and the operators go through a native module first (csrc/fff_torch.cpp), which makes
 the same checks and the call in well under a microsecond; a call it does not recognise as ordinary
 comes back unmade (-1) and takes the checks below, which say what is wrong with it.  Everything
 else is ctypes."""
@@ -118,6 +118,7 @@ _native_module = None
 class _NotBuilt:
     """In the place of the native module where torch came without its headers: no call is ordinary."""
     forward_hard = moe_top1_forward = forward_soft = forward_block = staticmethod(lambda *args: -1)
+    moe_route = moe_route_backward = mx4_quantize = mx4_dequantize = mx4_product = leaf_forward_mx4 = forward_hard
 
 
 def _native():
@@ -347,6 +348,11 @@ def fff_moe_route(logits, k, expert_idx, weight, count=None, prob_mean=None, los
     """The k experts of every token of logits [T, E] -> expert_idx [T, k] int32, weight [T, k] float32; with any of count [E + 1]
     int32, prob_mean [E] and loss [2] float32 also what the tokens have in common: tokens per expert (and in all), mean probabilities,
     the balance loss and the z loss.  token_mask [T] uint8 or bool: tokens that take part."""
+    rc = (_native_module or _native()).moe_route(logits, k, expert_idx, weight, count, prob_mean, loss, token_mask, normalise, stream)
+    if rc == 0:
+        return
+    if rc > 0:
+        raise FffError(rc, "fff_moe_route")
     import torch
     where = "fff_moe_route"
     T, E = _size(where, "logits", logits, (2,))
@@ -372,6 +378,11 @@ def fff_route_scratch_bytes(T: int, n_experts: int) -> int:
 def fff_moe_route_backward(logits, expert_idx, count, dlogits, dweight=None, dloss=None, token_mask=None, normalise=True, stream=None) -> None:
     """dlogits [T, E] from the gradients of fff_moe_route's weights (dweight [T, k]) and losses (dloss [2], on the GPU), float32 both; expert_idx
     and count as that call wrote them."""
+    rc = (_native_module or _native()).moe_route_backward(logits, expert_idx, count, dlogits, dweight, dloss, token_mask, normalise, stream)
+    if rc == 0:
+        return
+    if rc > 0:
+        raise FffError(rc, "fff_moe_route_backward")
     import torch
     where = "fff_moe_route_backward"
     T, E = _size(where, "logits", logits, (2,))
@@ -394,6 +405,11 @@ def _mx4_blocks(n: int) -> int:
 def fff_mx4_quantize(src, codes, scales, transpose=False, stream=None) -> None:
     """src [rows, cols] or [batch, rows, cols] -> four-bit codes [..., rows, 16 ceil(cols / 32)] and scales [..., rows, ceil(cols / 32)],
     uint8 both; with transpose those of the columns, [..., cols, 16 ceil(rows / 32)] and [..., cols, ceil(rows / 32)]."""
+    rc = (_native_module or _native()).mx4_quantize(src, codes, scales, transpose, stream)
+    if rc == 0:
+        return
+    if rc > 0:
+        raise FffError(rc, "fff_mx4_quantize")
     import torch
     where = "fff_mx4_quantize"
     shape = _size(where, "src", src, (2, 3))
@@ -408,6 +424,11 @@ def fff_mx4_quantize(src, codes, scales, transpose=False, stream=None) -> None:
 
 def fff_mx4_dequantize(codes, scales, out, stream=None) -> None:
     """out [..., rows, cols] <- the values of codes [..., rows, 16 ceil(cols / 32)] and scales [..., rows, ceil(cols / 32)]."""
+    rc = (_native_module or _native()).mx4_dequantize(codes, scales, out, stream)
+    if rc == 0:
+        return
+    if rc > 0:
+        raise FffError(rc, "fff_mx4_dequantize")
     import torch
     where = "fff_mx4_dequantize"
     shape = _size(where, "out", out, (2, 3))
@@ -422,6 +443,11 @@ def fff_mx4_dequantize(codes, scales, out, stream=None) -> None:
 def fff_mx4_product(a, w_codes, w_scales, out, a_scales=None, bias=None, act=ACT_NONE, stream=None) -> None:
     """out [T, N] = act(A W^T + bias) with W [N, K] in four bits; a [T, K] bfloat16, or with a_scales the codes of such rows.  K is
     that of a in bfloat16; of codes, what their whole blocks hold (the codes behind a row's end are zeros)."""
+    rc = (_native_module or _native()).mx4_product(a, w_codes, w_scales, out, a_scales, bias, act, stream)
+    if rc == 0:
+        return
+    if rc > 0:
+        raise FffError(rc, "fff_mx4_product")
     import torch
     where = "fff_mx4_product"
     T, K = _size(where, "a", a, (2,))
@@ -453,6 +479,11 @@ def fff_leaf_forward_mx4(x, leaf_w1, leaf_s1, leaf_b1, leaf_w2, leaf_s2, leaf_b2
     """out [T, O] = the networks of the leaves leaf_idx [T, k] (or [T]) of every token of x [T, D], with their matrices in four bits, times
     weight [T, k] (or [T]; None: ones) and added up.  leaf_w1, leaf_s1 are codes and scales of [leaves, width, D], leaf_w2, leaf_s2
     of [leaves, O, width]; leaf_b1 [leaves, width]; leaf_b2 [leaves, O]."""
+    rc = (_native_module or _native()).leaf_forward_mx4(x, leaf_w1, leaf_s1, leaf_b1, leaf_w2, leaf_s2, leaf_b2, leaf_idx, weight, act, out, stream)
+    if rc == 0:
+        return
+    if rc > 0:
+        raise FffError(rc, "fff_leaf_forward_mx4")
     import torch
     where = "fff_leaf_forward_mx4"
     T, D = _rows(where, "x", x)

@@ -13,8 +13,11 @@
 namespace fff {
 namespace {
 
-constexpr int kRouteWaves = 4;
-constexpr int kMaxRouteBlocks = 512;
+constexpr int kBackwardWaves = 4;
+constexpr int kMaxBackwardBlocks = 2048;
+// Waves of a block of the forward kernel: as many as its sums of p per wave leave room for in LDS and its registers on a compute unit, since a
+// block leaves one row of partial sums (sixteen waves a block on 256 blocks instead of four on 512, 512 experts: 92 -> 45 us).
+constexpr int route_waves(int V) { return V == 8 ? 16 : V == 16 ? 8 : 4; }
 
 struct RouteArgs {
     const void* logits;
@@ -39,6 +42,9 @@ template <int CTRL> __device__ __forceinline__ float dpp(float v) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
 }
 template <int CTRL> __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false); }
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
+__device__ __forceinline__ uint32_t word(uint32_t v) { return v; }
+__device__ __forceinline__ void unword(uint32_t w, uint32_t& v) { v = w; }
 __device__ __forceinline__ uint32_t word(float v) { return __float_as_uint(v); }
 __device__ __forceinline__ uint32_t word(int v) { return (uint32_t)v; }
 __device__ __forceinline__ void unword(uint32_t w, float& v) { v = __uint_as_float(w); }
@@ -68,6 +74,7 @@ template <class T, class OP> __device__ __forceinline__ T group_reduce(T v, int 
 }
 __device__ __forceinline__ float group_max(float v, int G) { return group_reduce(v, G, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float group_add(float v, int G) { return group_reduce(v, G, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ uint32_t group_max(uint32_t v, int G) { return group_reduce(v, G, [](uint32_t a, uint32_t b) { return max(a, b); }); }
 __device__ __forceinline__ int group_min(int v, int G) { return group_reduce(v, G, [](int a, int b) { return min(a, b); }); }
 
 // Element of the row that register v of lane gi holds: whole pieces of 16 bytes, lane after lane, or (VEC = false: rows that
@@ -118,32 +125,103 @@ __device__ __forceinline__ float relative(float l, float m) {
 // order of LDS accesses within a wave (they execute in order; the compiler must keep them so)
 __device__ __forceinline__ void wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+// One by one the largest logits that a group holds; values of -infinity are none.
+//
+// bf16 logits: value and index are one 32-bit key (the value's bits in the order of values, then the index turned round), so that the
+// largest key is the choice, ties included.  fp32: the lane whose largest value is the group's takes it from its registers; only where two
+// lanes hold it the lower index is looked for.
+template <bool BF16, int V, bool VEC> struct Picker {
+    float l[V];
+    uint32_t key[BF16 ? V : 1];
+    float mine;
+    __device__ __forceinline__ Picker(const float (&row)[V], int gi, int G) {
+        if constexpr (BF16) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const uint32_t b = __float_as_uint(row[v] + 0.0f);            // (-0 as 0)
+                const uint32_t up = (b & 0x80000000u) ? ~b : b | 0x80000000u;
+                key[v] = row[v] > -__builtin_inff() ? (up & 0xffff0000u) | (0xffffu - (uint32_t)element<BF16, VEC>(v, gi, G)) : 0u;
+            }
+        } else {
+            mine = -__builtin_inff();
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                l[v] = row[v];
+                mine = fmaxf(mine, l[v]);
+            }
+        }
+    }
+    // Whether there is one; its value; `at`: its index, in the one lane that answers true.
+    __device__ __forceinline__ bool next(int gi, int G, float* value, int* at, bool* found) {
+        if constexpr (BF16) {
+            uint32_t best = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) best = max(best, key[v]);
+            best = group_max(best, G);
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0u : key[v];
+            *found = best != 0;
+            *at = 0xffff - (int)(best & 0xffffu);
+            const uint32_t up = best & 0xffff0000u;
+            *value = __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up & 0xffff0000u);
+            return gi == 0 && *found;
+        } else {
+            const float ninf = -__builtin_inff();
+            const float best = group_max(mine, G);
+            *value = best;
+            *found = best > ninf;
+            bool have = mine == best && *found;
+            if (__popcll(__ballot(have)) != __popcll(__ballot(*found && gi == 0))) {     // two lanes hold it somewhere
+                int lowest = 0x7fffffff;
+#pragma unroll
+                for (int v = V - 1; v >= 0; --v)
+                    if (l[v] == best) lowest = element<BF16, VEC>(v, gi, G);
+                const int first = group_min(have ? lowest : 0x7fffffff, G);       // (of all lanes)
+                have = have && lowest == first;
+            }
+            if (have) {
+                bool taken = false;
+                mine = ninf;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const bool hit = l[v] == best && !taken;
+                    *at = hit ? element<BF16, VEC>(v, gi, G) : *at;
+                    l[v] = hit ? ninf : l[v];
+                    taken = taken || hit;
+                    mine = fmaxf(mine, l[v]);
+                }
+            }
+            return have;
+        }
+    }
+};
+
 template <bool BF16, int V, bool VEC>
-__global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs a) {
-    extern __shared__ float lds[];               // statistics: kRouteWaves x E sums, E counts
-    __shared__ float pick_w[64 * kRouteWaves * 8];
-    __shared__ int32_t pick_i[64 * kRouteWaves * 8];
-    __shared__ float block_z[kRouteWaves];
-    __shared__ int32_t block_n[kRouteWaves];
+__global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteArgs a) {
+    constexpr int kWaves = route_waves(V);
+    extern __shared__ float lds[];               // the slots chosen; statistics: kWaves x E sums, E counts
+    __shared__ float block_z[kWaves];
+    __shared__ int32_t block_n[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int G = a.lanes, gi = lane & (G - 1), rows = 64 / G, E = a.E, k = a.k;
     const bool stats = a.part_p != nullptr;
-    int32_t* const counts = (int32_t*)(lds + kRouteWaves * E);
-    // slots of this group: k <= E <= G V and k <= 32
-    float* const my_w = pick_w + (tid / G) * k;
-    int32_t* const my_i = pick_i + (tid / G) * k;
+    const int slots = kWaves * rows * k;
+    float* const my_w = lds + (tid / G) * k;
+    int32_t* const my_i = (int32_t*)lds + slots + (tid / G) * k;
+    float* const sums = lds + 2 * slots;
+    int32_t* const counts = (int32_t*)sums + kWaves * E;
     const float ninf = -__builtin_inff();
     float acc[V], z = 0;
     int n = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[v] = 0;
     if (stats) {
-        for (int e = tid; e < E; e += 64 * kRouteWaves) counts[e] = 0;
+        for (int e = tid; e < E; e += 64 * kWaves) counts[e] = 0;
         __syncthreads();
     }
-    const int64_t step = (int64_t)gridDim.x * kRouteWaves * rows;
+    const int64_t step = (int64_t)gridDim.x * kWaves * rows;
     // (rows past the end and masked ones run along as empty rows: the lanes of a wave stay together)
-    for (int64_t t0 = ((int64_t)blockIdx.x * kRouteWaves + wv) * rows; t0 < a.T; t0 += step) {
+    for (int64_t t0 = ((int64_t)blockIdx.x * kWaves + wv) * rows; t0 < a.T; t0 += step) {
         const int64_t t = t0 + lane / G;
         const bool there = t < a.T, on = there && (!a.mask || a.mask[t]);
         float l[V];
@@ -156,47 +234,36 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs
         }
         m = group_max(m, G);
         const bool any = m > ninf;
-        if (stats) {
-            float p[V], s = 0;
+        float total = 0;
+        if (stats || !a.normalise) {
+            float p[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 p[v] = any ? relative(l[v], m) : 0.0f;
-                s += p[v];
+                total += p[v];
             }
-            s = group_add(s, G);
-            const float inv = any ? 1.0f / s : 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] = fmaf(p[v], inv, acc[v]);
-            if (any && gi == 0) {
-                const float lse = m + logf(s);
-                z = fmaf(lse, lse, z);
-                ++n;
-            }
-        }
-        float total = 0;
-        if (!a.normalise) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) total += any ? relative(l[v], m) : 0.0f;
             total = group_add(total, G);
+            if (stats) {
+                const float inv = any ? 1.0f / total : 0.0f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] = fmaf(p[v], inv, acc[v]);
+                if (any && gi == 0) {
+                    const float lse = m + logf(total);
+                    z = fmaf(lse, lse, z);
+                    ++n;
+                }
+            }
         }
+        Picker<BF16, V, VEC> picker(l, gi, G);
         float chosen = 0;
         for (int i = 0; i < k; ++i) {
-            float best = ninf;
-#pragma unroll
-            for (int v = 0; v < V; ++v) best = fmaxf(best, l[v]);
-            best = group_max(best, G);
-            int at = 0x7fffffff;
-#pragma unroll
-            for (int v = V - 1; v >= 0; --v)
-                if (l[v] == best) at = element<BF16, VEC>(v, gi, G);
-            at = group_min(at, G);
-            const bool found = best > ninf;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (element<BF16, VEC>(v, gi, G) == at) l[v] = ninf;
-            const float w = found ? relative(best, m) : 0.0f;
+            float value;
+            int at = 0;
+            bool found;
+            const bool mine = picker.next(gi, G, &value, &at, &found);
+            const float w = found ? relative(value, m) : 0.0f;
             chosen += w;
-            if (gi == 0) {
+            if (mine || (!found && gi == 0)) {
                 my_w[i] = w;
                 my_i[i] = found ? at : -1;
                 if (stats && found) atomicAdd(counts + at, 1);
@@ -225,7 +292,7 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int e = element<BF16, VEC>(v, gi, G);
-            if (e < E) lds[wv * E + e] = acc[v];
+            if (e < E) sums[wv * E + e] = acc[v];
         }
     }
     if (lane == 0) {
@@ -233,42 +300,49 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs
         block_n[wv] = n;
     }
     __syncthreads();
-    for (int e = tid; e < E; e += 64 * kRouteWaves) {
-        float s = lds[e];
+    for (int e = tid; e < E; e += 64 * kWaves) {
+        float s = sums[e];
 #pragma unroll
-        for (int w = 1; w < kRouteWaves; ++w) s += lds[w * E + e];
+        for (int w = 1; w < kWaves; ++w) s += sums[w * E + e];
         a.part_p[(int64_t)blockIdx.x * E + e] = s;
         a.part_count[(int64_t)blockIdx.x * E + e] = counts[e];
     }
     if (tid == 0) {
-        a.part_z[blockIdx.x] = (block_z[0] + block_z[1]) + (block_z[2] + block_z[3]);
-        a.part_n[blockIdx.x] = (block_n[0] + block_n[1]) + (block_n[2] + block_n[3]);
+        z = 0;
+        n = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            z += block_z[w];
+            n += block_n[w];
+        }
+        a.part_z[blockIdx.x] = z;
+        a.part_n[blockIdx.x] = n;
         if (blockIdx.x == 0) *a.ticket = 0;
     }
 }
 
-// 64 experts a block: sums over the rows of the first launch, then (the block that comes last) the losses.
-__global__ __launch_bounds__(256) void route_finish_kernel(const float* __restrict__ part_p, const int32_t* __restrict__ part_count,
-                                                           const float* __restrict__ part_z, const int32_t* __restrict__ part_n, int blocks,
-                                                           int E, int k, int32_t* __restrict__ count, float* __restrict__ prob_mean,
-                                                           float* __restrict__ loss, float* __restrict__ share, int32_t* __restrict__ ticket) {
-    __shared__ float sum_p[4][64];
-    __shared__ int32_t sum_c[4][64];
-    __shared__ float sum_z[4];
-    __shared__ int32_t sum_n[4];
-    __shared__ bool last;
+// 64 experts a block: sums over the rows of the first launch (sixteen waves, every sixteenth row each), then (the block that comes last) the losses.
+constexpr int kFinishWaves = 16;
+__global__ __launch_bounds__(64 * kFinishWaves) void route_finish_kernel(const float* __restrict__ part_p, const int32_t* __restrict__ part_count,
+                                                                         const float* __restrict__ part_z, const int32_t* __restrict__ part_n,
+                                                                         int blocks, int E, int k, int32_t* __restrict__ count,
+                                                                         float* __restrict__ prob_mean, float* __restrict__ loss,
+                                                                         float* __restrict__ share, int32_t* __restrict__ ticket) {
+    __shared__ float sum_p[kFinishWaves][64], sum_z[kFinishWaves];
+    __shared__ int32_t sum_c[kFinishWaves][64], sum_n[kFinishWaves];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int e = blockIdx.x * 64 + lane;
     float p = 0, z = 0;
     int32_t c = 0, n = 0;
-    if (e < E)
-        for (int b = wv; b < blocks; b += 4) {
+    if (e < E) {
+#pragma unroll 8
+        for (int b = wv; b < blocks; b += kFinishWaves) {
             p += part_p[(int64_t)b * E + e];
             c += part_count[(int64_t)b * E + e];
         }
-    for (int b = tid; b < blocks; b += 256) {
-        z += part_z[b];
-        n += part_n[b];
+    }
+    if (tid < blocks) {           // (no more blocks than threads)
+        z = part_z[tid];
+        n = part_n[tid];
     }
     for (int d = 1; d < 64; d <<= 1) {
         z += __shfl_xor(z, d, 64);
@@ -281,30 +355,36 @@ __global__ __launch_bounds__(256) void route_finish_kernel(const float* __restri
         sum_n[wv] = n;
     }
     __syncthreads();
-    z = (sum_z[0] + sum_z[1]) + (sum_z[2] + sum_z[3]);
-    n = (sum_n[0] + sum_n[1]) + (sum_n[2] + sum_n[3]);
-    if (wv == 0) {
-        p = (sum_p[0][lane] + sum_p[1][lane]) + (sum_p[2][lane] + sum_p[3][lane]);
-        c = (sum_c[0][lane] + sum_c[1][lane]) + (sum_c[2][lane] + sum_c[3][lane]);
-        const float mean = n > 0 ? p / (float)n : 0.0f;
-        if (e < E) {
-            if (count) count[e] = c;
-            if (prob_mean) prob_mean[e] = mean;
-        }
-        if (blockIdx.x == 0 && lane == 0 && count) count[E] = n;
-        float f = e < E && n > 0 ? (float)c / ((float)n * (float)k) * mean : 0.0f;
-        f = wave_sum(f);
-        if (lane == 0 && loss) {
-            __hip_atomic_store(share + blockIdx.x, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    if (wv != 0) return;
+    z = sum_z[0];
+    n = sum_n[0];
+    p = sum_p[0][lane];
+    c = sum_c[0][lane];
+#pragma unroll
+    for (int w = 1; w < kFinishWaves; ++w) {
+        z += sum_z[w];
+        n += sum_n[w];
+        p += sum_p[w][lane];
+        c += sum_c[w][lane];
+    }
+    const float mean = n > 0 ? p / (float)n : 0.0f;
+    if (e < E) {
+        if (count) count[e] = c;
+        if (prob_mean) prob_mean[e] = mean;
+    }
+    if (blockIdx.x == 0 && lane == 0 && count) count[E] = n;
+    if (!loss) return;
+    const float f = wave_sum(e < E && n > 0 ? (float)c / ((float)n * (float)k) * mean : 0.0f);
+    if (lane == 0) {
+        __hip_atomic_store(share + blockIdx.x, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const bool last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+        if (last) {
+            float s = 0;
+            for (int b = 0; b < (int)gridDim.x; ++b) s += __hip_atomic_load(share + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            loss[0] = (float)E * s;
+            loss[1] = n > 0 ? z / (float)n : 0.0f;
         }
     }
-    __syncthreads();
-    if (!loss || !last || tid != 0) return;
-    float s = 0;
-    for (int b = 0; b < (int)gridDim.x; ++b) s += __hip_atomic_load(share + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    loss[0] = (float)E * s;
-    loss[1] = n > 0 ? z / (float)n : 0.0f;
 }
 
 // what a call without tokens leaves
@@ -316,11 +396,15 @@ __global__ __launch_bounds__(256) void route_empty_kernel(int E, int32_t* __rest
 }
 
 template <bool BF16, int V, bool VEC>
-__global__ __launch_bounds__(64 * kRouteWaves) void route_backward_kernel(const RouteArgs a) {
+__global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(const RouteArgs a) {
+    extern __shared__ float patches[];           // G V words a group, zeros between rows
     constexpr int VE = BF16 ? 8 : 4, es = BF16 ? 2 : 4;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int G = a.lanes, gi = lane & (G - 1), rows = 64 / G, E = a.E, k = a.k;
     const float ninf = -__builtin_inff();
+    float* const patch = patches + (tid / G) * (G * V);
+    for (int i = lane; i < 64 * V; i += 64) patches[wv * 64 * V + i] = 0;
+    wave_sync();
     float pull[V], pull_z = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) pull[v] = 0;
@@ -336,8 +420,8 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_backward_kernel(const 
             }
         }
     }
-    const int64_t step = (int64_t)gridDim.x * kRouteWaves * rows;
-    for (int64_t t0 = ((int64_t)blockIdx.x * kRouteWaves + wv) * rows; t0 < a.T; t0 += step) {
+    const int64_t step = (int64_t)gridDim.x * kBackwardWaves * rows;
+    for (int64_t t0 = ((int64_t)blockIdx.x * kBackwardWaves + wv) * rows; t0 < a.T; t0 += step) {
         const int64_t t = t0 + lane / G;
         const bool there = t < a.T, on = there && (!a.mask || a.mask[t]);
         const int64_t tt = there ? t : a.T - 1;
@@ -365,32 +449,42 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_backward_kernel(const 
         const float zz = any && pull_z != 0.0f ? pull_z * (m + logf(s)) : 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) d[v] = l[v] > 0.0f ? l[v] * inv * (pull[v] - dot + zz) : 0.0f;
-        if (a.dweight && any) {
-            // the chosen experts' shares, then their part of the gradient
+        if (a.dweight) {
+            // The slots' part: a lane a slot, put to where the expert's lane reads it.  (Rows that take no part run along.)
             const char* const row = (const char*)a.logits + tt * E * es;
             float sum = 0, mean = 0;
-            for (int i = 0; i < k; ++i) {
-                const uint32_t e = (uint32_t)a.idx[tt * k + i];
+            for (int i = gi; i < k; i += G) {
+                const uint32_t e = any ? (uint32_t)a.idx[tt * k + i] : ~0u;
                 if (e >= (uint32_t)E) continue;
                 const float x = Elem<BF16>::load(row, e);
                 const float w = x == x ? relative(x, m) : 0.0f;
                 sum += w;
                 mean = fmaf(w, a.dweight[tt * k + i], mean);
             }
+            sum = group_add(sum, G);
+            mean = group_add(mean, G);
             const float by = a.normalise ? (sum > 0.0f ? 1.0f / sum : 0.0f) : inv;
             mean *= by;
             if (!a.normalise) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) d[v] = fmaf(-l[v] * inv, mean, d[v]);
             }
-            for (int i = 0; i < k; ++i) {
-                const int e = a.idx[tt * k + i];
-                if ((uint32_t)e >= (uint32_t)E) continue;
-                const float g = a.dweight[tt * k + i] - (a.normalise ? mean : 0.0f);
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (element<BF16, VEC>(v, gi, G) == e) d[v] = fmaf(l[v] * by, g, d[v]);
+            for (int i = gi; i < k; i += G) {
+                const uint32_t e = any ? (uint32_t)a.idx[tt * k + i] : ~0u;
+                if (e >= (uint32_t)E) continue;
+                const float x = Elem<BF16>::load(row, e);
+                const float w = x == x ? relative(x, m) : 0.0f;
+                atomicAdd(patch + e, w * by * (a.dweight[tt * k + i] - (a.normalise ? mean : 0.0f)));
             }
+            wave_sync();
+#pragma unroll
+            for (int v = 0; v < V; ++v) d[v] += patch[element<BF16, VEC>(v, gi, G)];
+            wave_sync();
+            for (int i = gi; i < k; i += G) {
+                const uint32_t e = any ? (uint32_t)a.idx[tt * k + i] : ~0u;
+                if (e < (uint32_t)E) patch[e] = 0;
+            }
+            wave_sync();
         }
         if (!there) continue;
         char* const out = (char*)a.dlogits + t * E * es;
@@ -418,11 +512,12 @@ void route_shape(int64_t E, int* V, int* G) {
     *G = g;
 }
 
-// A block's share of the tokens: enough blocks to cover the chip, but no more rows of partial sums than they are worth.
-int route_blocks(int64_t T, int G) {
-    const int64_t rows = kRouteWaves * (64 / G);
+// Rows of partial sums that scratch has room for, and blocks of the forward kernel at most: one a compute unit.
+constexpr int64_t kMaxPartRows = 256;
+int route_blocks(int64_t T, int V, int G) {
+    const int64_t rows = route_waves(V) * (64 / G), most = device_info().cus < kMaxPartRows ? device_info().cus : kMaxPartRows;
     const int64_t b = (T + rows - 1) / rows;
-    return (int)(b > kMaxRouteBlocks ? kMaxRouteBlocks : b);
+    return (int)(b > most ? most : b);
 }
 
 template <class F> hipError_t with_shape(bool bf16, int V, bool vec, F f) {
@@ -438,12 +533,11 @@ template <class F> hipError_t with_shape(bool bf16, int V, bool vec, F f) {
     return bf16 ? type(std::true_type()) : type(std::false_type());
 }
 
+
 struct RouteScratch {
     int64_t part_p, part_count, part_z, part_n, share, ticket, total;
     RouteScratch(int64_t T, int64_t E) {
-        int V, G;
-        route_shape(E, &V, &G);
-        const int64_t blocks = T > 0 ? route_blocks(T, G) : 0;
+        const int64_t blocks = T > 0 ? (T < kMaxPartRows ? T : kMaxPartRows) : 0;
         int64_t o = 0;
         const auto take = [&](int64_t words) {
             const int64_t at = o;
@@ -500,21 +594,21 @@ hipError_t launch_route(const Route& r, int32_t* idx, float* weight, int32_t* co
         a.part_n = (int32_t*)(base + at.part_n);
         a.ticket = (int32_t*)(base + at.ticket);
     }
-    const int blocks = route_blocks(r.T, a.lanes);
-    const size_t lds = stats ? (size_t)(kRouteWaves + 1) * r.E * 4 : 0;
+    const int blocks = route_blocks(r.T, V, a.lanes), waves = route_waves(V);
+    const size_t lds = (size_t)waves * (64 / a.lanes) * r.k * 8 + (stats ? (size_t)(waves + 1) * r.E * 4 : 0);
     note_launch("route_kernel<%s,%d,%s>", r.bf16 ? "bf16" : "f32", V, vec ? "pieces" : "elements");
     hipError_t e = with_shape(r.bf16, V, vec, [&](auto B, auto N, auto X) {
         const auto kernel = route_kernel<decltype(B)::value, decltype(N)::value, decltype(X)::value>;
-        if (lds > 32 * 1024) {
+        if (lds > 60 * 1024) {
             const hipError_t rc = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (rc != hipSuccess) return rc;
         }
-        kernel<<<dim3((unsigned)blocks), 64 * kRouteWaves, lds, s>>>(a);
+        kernel<<<dim3((unsigned)blocks), 64 * waves, lds, s>>>(a);
         return hipGetLastError();
     });
     if (e != hipSuccess || !stats) return e;
     note_launch("route_finish_kernel");
-    route_finish_kernel<<<dim3((unsigned)((r.E + 63) / 64)), 256, 0, s>>>(a.part_p, a.part_count, a.part_z, a.part_n, blocks, a.E, a.k, count,
+    route_finish_kernel<<<dim3((unsigned)((r.E + 63) / 64)), 64 * kFinishWaves, 0, s>>>(a.part_p, a.part_count, a.part_z, a.part_n, blocks, a.E, a.k, count,
                                                                           prob_mean, loss, (float*)(base + at.share), a.ticket);
     return hipGetLastError();
 }
@@ -530,12 +624,18 @@ hipError_t launch_route_backward(const Route& r, const int32_t* idx, const int32
     a.dweight = dweight;
     a.dloss = dloss;
     a.dlogits = dlogits;
-    const int64_t rows = kRouteWaves * (64 / a.lanes);
+    const int64_t rows = kBackwardWaves * (64 / a.lanes);
     int64_t blocks = (r.T + rows - 1) / rows;
-    if (blocks > 4 * kMaxRouteBlocks) blocks = 4 * kMaxRouteBlocks;
+    if (blocks > kMaxBackwardBlocks) blocks = kMaxBackwardBlocks;
     note_launch("route_backward_kernel<%s,%d,%s>", r.bf16 ? "bf16" : "f32", V, vec ? "pieces" : "elements");
     return with_shape(r.bf16, V, vec, [&](auto B, auto N, auto X) {
-        route_backward_kernel<decltype(B)::value, decltype(N)::value, decltype(X)::value><<<dim3((unsigned)blocks), 64 * kRouteWaves, 0, s>>>(a);
+        const auto kernel = route_backward_kernel<decltype(B)::value, decltype(N)::value, decltype(X)::value>;
+        const size_t lds = (size_t)kBackwardWaves * 64 * decltype(N)::value * 4;
+        if (lds > 60 * 1024) {
+            const hipError_t rc = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (rc != hipSuccess) return rc;
+        }
+        kernel<<<dim3((unsigned)blocks), 64 * kBackwardWaves, lds, s>>>(a);
         return hipGetLastError();
     });
 }

@@ -27,7 +27,7 @@ __device__ __forceinline__ void load_to_lds_from(const char* base, uint32_t offs
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
-enum { kDense, kHidden, kOutput, kHiddenDirect, kOutputDirect };
+enum { kDense, kHidden, kOutput };
 
 struct Args {
     const char* a;               // rows of bf16, or codes
@@ -152,9 +152,25 @@ __device__ __forceinline__ float bias_at(const Args& a, const void* bias, int64_
     return a.out_bf16 ? bf16_to_f32(((const uint16_t*)bias)[n]) : ((const float*)bias)[n];
 }
 
-// The activation; GELU of results that end in bf16 by the polynomial whose error (5e-7) is far below that rounding: the library's error function
-// took a fifth of a 4096 x 4096 x 4096 product's time.
-__device__ __forceinline__ float apply(float v, int act, bool bf16) { return act == 2 ? v : bf16 ? activate_bulk(v, act) : activate(v, act); }
+// GELU of results that end in bf16: v Phi(v) by erfc(z) = (1 + a1 z + ... + a6 z^6)^-16, z = |v| / sqrt 2 >= 0 (Abramowitz & Stegun 7.1.28, absolute
+// error 3e-7; with the roundings of the sixteenth power under 2e-6), far below that rounding.  The library's error function took a fifth of a 4096 x 4096 x 4096
+// product's time, and one that needs an exponential (activate_bulk) a quarter more than this.
+__device__ __forceinline__ float gelu_bulk(float v) {
+    const float z = fabsf(v) * 0.70710678118654752440f;
+    float p = fmaf(z, 0.0000430638f, 0.0002765672f);
+    p = fmaf(p, z, 0.0001520143f);
+    p = fmaf(p, z, 0.0092705272f);
+    p = fmaf(p, z, 0.0422820123f);
+    p = fmaf(p, z, 0.0705230784f);
+    p = fmaf(p, z, 1.0f);
+    p *= p;
+    p *= p;
+    p *= p;
+    p *= p;
+    const float e = __builtin_amdgcn_rcpf(p);
+    return 0.5f * v * (v >= 0.0f ? 2.0f - e : e);
+}
+__device__ __forceinline__ float apply(float v, int act, bool bf16) { return act == 2 ? v : act == 1 && bf16 ? gelu_bulk(v) : activate(v, act); }
 
 // sixteen bytes at any address
 __device__ __forceinline__ uint4 load_bytes(const uint8_t* p) {
@@ -209,8 +225,6 @@ __device__ __forceinline__ void store8(char* out, bool bf16, bool vec, int64_t a
 //   kDense         rows of A as they come, rows of out too
 //   kHidden        a tile of one leaf's slots: rows of A are the slots' tokens; out is h [slot][32 blocks]
 //   kOutput        a tile of one leaf's slots: rows of A are h; out is y [pair] in fp32, or with k = 1 the token's row
-//   kHiddenDirect  a tile is one pair: h [pair], times the pair's weight
-//   kOutputDirect  a tile is one token: the sum over its pairs as one product along k rows of h and of W
 template <bool A4, int MT, int MODE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
     __shared__ f32x4_t part[WAVES][MT][kWave];
@@ -224,14 +238,11 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
     if constexpr (MODE == kDense) {
         first = tile * (16 * MT);
         rows = a.T - first;
-    } else if constexpr (MODE == kHidden || MODE == kOutput) {
+    } else {
         if (tile >= *a.n_tiles) return;
         leaf = a.tile_leaf[tile];
         first = a.tile_slot[tile];
         rows = a.start[leaf + 1] - first;
-    } else {
-        first = tile;
-        rows = 1;
     }
     if (rows > 16 * MT) rows = 16 * MT;
     f32x4_t acc[MT];
@@ -239,35 +250,15 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
     for (int m = 0; m < MT; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const char* a_row[MT];
     const uint8_t* as_row[MT];
-    if constexpr (MODE == kOutputDirect) {
-        // step c of pair i is step i * steps + c of the sum, so that waves that pair i leaves without a step begin with pair i + 1
-        const int steps = (a.Kb + 3) / 4;
-        for (int i = 0; i < a.k; ++i) {
-            const int64_t pair = first * a.k + i;
-            const uint32_t e = (uint32_t)a.idx[pair];
-            if (e >= a.E) continue;
-            a_row[0] = a.a + pair * a.a_row;
-            wave_steps<A4, MT>(a.w + ((int64_t)e * a.N + n) * w_row_bytes, a.w_scales + ((int64_t)e * a.N + n) * a.Kb, a_row, as_row, a.Kb, a.pieces,
-                               g, (wv + WAVES - i * steps % WAVES) % WAVES, WAVES, acc);
-        }
-    } else {
-        if constexpr (MODE == kHiddenDirect) {
-            const uint32_t e = (uint32_t)a.idx[first];
-            if (e >= a.E) return;              // (kOutputDirect does not read its row)
-            leaf = e;
-        }
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            int64_t r = 16 * m + j < rows ? 16 * m + j : rows - 1;
-            r += first;
-            if constexpr (MODE == kHidden) r = a.perm[r] / a.k;
-            if constexpr (MODE == kHiddenDirect) r = first / a.k;
-            a_row[m] = a.a + r * a.a_row;
-            as_row[m] = A4 ? a.a_scales + r * a.Kb : nullptr;
-        }
-        wave_steps<A4, MT>(a.w + (leaf * a.N + n) * w_row_bytes, a.w_scales + (leaf * a.N + n) * a.Kb, a_row, as_row, a.Kb, a.pieces, g, wv,
-                           WAVES, acc);
+    for (int m = 0; m < MT; ++m) {
+        int64_t r = 16 * m + j < rows ? 16 * m + j : rows - 1;
+        r += first;
+        if constexpr (MODE == kHidden) r = a.perm[r] / a.k;
+        a_row[m] = a.a + r * a.a_row;
+        as_row[m] = A4 ? a.a_scales + r * a.Kb : nullptr;
     }
+    wave_steps<A4, MT>(a.w + (leaf * a.N + n) * w_row_bytes, a.w_scales + (leaf * a.N + n) * a.Kb, a_row, as_row, a.Kb, a.pieces, g, wv, WAVES, acc);
 #pragma unroll
     for (int m = 0; m < MT; ++m) part[wv][m][lane] = acc[m];
     __syncthreads();
@@ -283,37 +274,23 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bias_at(a, a.bias, n4 + q), a.act, a.out_bf16) : 0.f;
             store4(a.out, a.out_bf16, a.out_vec, (first + row) * a.out_row, n4, a.N, o);
-        } else if constexpr (MODE == kHidden || MODE == kHiddenDirect) {
+        } else if constexpr (MODE == kHidden) {
             const uint16_t* const bias = (const uint16_t*)a.bias + leaf * a.N;
-            const float scale = MODE == kHiddenDirect && a.weight ? a.weight[first] : 1.0f;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bf16_to_f32(bias[n4 + q]), a.act, true) * scale : 0.f;
+            for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bf16_to_f32(bias[n4 + q]), a.act, true) : 0.f;
             // (the row of h is whole blocks of 32: zeros behind the leaf's width)
             store4(a.out, true, true, (first + row) * a.out_row, n4, a.out_row, o);
             if (n4 + 16 >= a.N && n4 + 16 < a.out_row) {
                 const float z[4] = {0.f, 0.f, 0.f, 0.f};
                 store4(a.out, true, true, (first + row) * a.out_row, n4 + 16, a.out_row, z);
             }
-        } else if constexpr (MODE == kOutput) {
+        } else {
             const uint16_t* const bias = (const uint16_t*)a.bias + leaf * a.N;
             const int64_t pair = a.perm[first + row];
             const float scale = a.k == 1 && a.weight ? a.weight[pair] : 1.0f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? (v[q] + bf16_to_f32(bias[n4 + q])) * scale : 0.f;
             store4(a.out, a.out_bf16, a.out_vec, pair * a.out_row, n4, a.N, o);
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = v[q];
-            for (int i = 0; i < a.k; ++i) {
-                const uint32_t e = (uint32_t)a.idx[first * a.k + i];
-                if (e >= a.E) continue;
-                const float scale = a.weight ? a.weight[first * a.k + i] : 1.0f;
-                const uint16_t* const bias = (const uint16_t*)a.bias + (int64_t)e * a.N;
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (n4 + q < a.N) o[q] = fmaf(scale, bf16_to_f32(bias[n4 + q]), o[q]);
-            }
-            store4(a.out, true, a.out_vec, first * a.out_row, n4, a.N, o);
         }
     }
 }
@@ -639,18 +616,19 @@ template <bool A4, int MODE> hipError_t launch_tiles(const Args& a, int64_t row_
 // dependent reads of weights.
 constexpr int kTokenWaves = 8, kTokenTiles = 4;
 
-// Steps c0, c0 + stride, ... of one row of A (in global memory or LDS) against up to kTokenTiles tiles of 16 rows of W.
-__device__ __forceinline__ void tiles_steps(const uint8_t* const (&w_row)[kTokenTiles], const uint8_t* const (&ws_row)[kTokenTiles], int tiles,
-                                            const char* a_row, int Kb, int pieces, int g, int c0, int stride, f32x4_t (&acc)[kTokenTiles]) {
+// Steps c0, c0 + stride, ... of one row of A (in global memory or LDS) against up to NT tiles of 16 rows of W.
+template <int NT>
+__device__ __forceinline__ void tiles_steps(const uint8_t* const (&w_row)[NT], const uint8_t* const (&ws_row)[NT], int tiles,
+                                            const char* a_row, int Kb, int pieces, int g, int c0, int stride, f32x4_t (&acc)[NT]) {
     const int steps = (Kb + 3) / 4;
     for (int c = c0; c < steps; c += stride) {
         const int b = 4 * c + g;
         const bool in = b < Kb;
         const int bb = in ? b : Kb - 1;
-        uint4 w[kTokenTiles], x[4];
-        uint32_t ws[kTokenTiles];
+        uint4 w[NT], x[4];
+        uint32_t ws[NT];
 #pragma unroll
-        for (int t = 0; t < kTokenTiles; ++t) {
+        for (int t = 0; t < NT; ++t) {
             if (t >= tiles) break;
             w[t] = *(const uint4*)(w_row[t] + 16 * (int64_t)bb);
             ws[t] = ws_row[t][bb];
@@ -661,7 +639,7 @@ __device__ __forceinline__ void tiles_steps(const uint8_t* const (&w_row)[kToken
             x[u] = keep_if(there, *(const uint4*)(a_row + 16 * (int64_t)(there ? 4 * bb + u : 0)));
         }
 #pragma unroll
-        for (int t = 0; t < kTokenTiles; ++t) {
+        for (int t = 0; t < NT; ++t) {
             if (t >= tiles) break;
             const uint4 v = keep_if(in, w[t]);
             const float s = __uint_as_float((in ? ws[t] : 0u) << 23);
@@ -754,6 +732,72 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
             }
         }
     }
+}
+
+// ---- few pairs of wide leaves ------------------------------------------------------------------------------
+//
+// Nothing to group: a block takes 16 NT columns of one pair's hidden activations (HIDDEN; h [pair], times the pair's weight) or of one token's
+// outputs (the sum over its pairs as one product along k rows of h and of W), K shared out among its waves.  Bound by the bytes of the weights.
+template <bool HIDDEN, int NT>
+__global__ __launch_bounds__(64 * kTokenWaves, 4) void mx4_direct_kernel(const Args a) {
+    __shared__ float part[kTokenWaves][16 * NT];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = lane & 15, g = lane >> 4;
+    const int64_t width = HIDDEN ? a.out_row : a.N, n_blocks = (width + 16 * NT - 1) / (16 * NT);
+    const int64_t item = blockIdx.x / n_blocks, n0 = (blockIdx.x - item * n_blocks) * (16 * NT);
+    const int k = HIDDEN ? 1 : a.k, steps = (a.Kb + 3) / 4;
+    if (HIDDEN && (uint32_t)a.idx[item] >= a.E) return;            // (nobody reads its row)
+    const int tiles = width - n0 < 16 * NT ? (int)((width - n0 + 15) / 16) : NT;
+    f32x4_t acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < k; ++i) {
+        const int64_t pair = item * k + i;
+        const uint32_t e = (uint32_t)a.idx[pair];
+        if (e >= a.E) continue;
+        const uint8_t *w_row[NT], *ws_row[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int64_t n = n0 + 16 * t + j, r = (int64_t)e * a.N + (n < a.N ? n : a.N - 1);
+            w_row[t] = a.w + r * a.Kb * 16;
+            ws_row[t] = a.w_scales + r * a.Kb;
+        }
+        // (step c of pair i is step i * steps + c of the sum: waves that pair i leaves without a step begin with pair i + 1)
+        tiles_steps<NT>(w_row, ws_row, tiles, a.a + (HIDDEN ? pair / a.k : pair) * a.a_row, a.Kb, a.pieces, g,
+                        (wv + kTokenWaves - i * steps % kTokenWaves) % kTokenWaves, kTokenWaves, acc);
+    }
+    if (j == 0) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *(f32x4_t*)&part[wv][16 * t + 4 * g] = acc[t];
+    }
+    __syncthreads();
+    const int64_t n = n0 + tid;
+    if (tid >= 16 * NT || n >= width) return;
+    float v = part[0][tid];
+#pragma unroll
+    for (int w = 1; w < kTokenWaves; ++w) v += part[w][tid];
+    for (int i = 0; i < k; ++i) {
+        const int64_t pair = item * k + i;
+        const uint32_t e = (uint32_t)a.idx[pair];
+        if (e >= a.E || n >= a.N) continue;
+        const float scale = a.weight ? a.weight[pair] : 1.0f, bias = bf16_to_f32(((const uint16_t*)a.bias)[(int64_t)e * a.N + n]);
+        v = HIDDEN ? apply(v + bias, a.act, true) * scale : fmaf(scale, bias, v);
+    }
+    if (HIDDEN && n >= a.N) v = 0.f;
+    ((uint16_t*)a.out)[item * a.out_row + n] = f32_to_bf16(v);
+}
+
+// Columns a block: 64 where that leaves a block for every compute unit.
+template <bool HIDDEN> hipError_t launch_direct(const Args& a, int64_t items, hipStream_t s) {
+    const int64_t width = HIDDEN ? a.out_row : a.N;
+    const auto blocks = [&](int nt) { return (width + 16 * nt - 1) / (16 * nt) * items; };
+    const int nt = blocks(4) >= device_info().cus ? 4 : blocks(2) >= device_info().cus ? 2 : 1;
+    if (blocks(nt) >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    note_launch("mx4_direct_kernel<%s,%d>", HIDDEN ? "hidden" : "output", nt);
+    const dim3 grid((unsigned)blocks(nt));
+    if (nt == 4) mx4_direct_kernel<HIDDEN, 4><<<grid, 64 * kTokenWaves, 0, s>>>(a);
+    else if (nt == 2) mx4_direct_kernel<HIDDEN, 2><<<grid, 64 * kTokenWaves, 0, s>>>(a);
+    else mx4_direct_kernel<HIDDEN, 1><<<grid, 64 * kTokenWaves, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 // ---- grouping of the pairs by leaf -------------------------------------------------------------------------
@@ -870,7 +914,7 @@ __global__ __launch_bounds__(256) void group_place_kernel(const int32_t* __restr
 }
 
 // All of it in one block, for few pairs: counts, sums and places in LDS (a second pass of atomics gives the places).
-constexpr int64_t kGroupOnePairs = 32768, kGroupOneLeaves = 4096;
+constexpr int64_t kGroupOnePairs = 4096, kGroupOneLeaves = 4096;
 __global__ __launch_bounds__(1024) void group_one_kernel(const int32_t* __restrict__ idx, int P, int E, int tile_rows, int32_t* __restrict__ start,
                                                          int32_t* __restrict__ tile_start, int32_t* __restrict__ perm, int32_t* __restrict__ tile_leaf,
                                                          int32_t* __restrict__ tile_slot) {
@@ -898,23 +942,39 @@ __global__ __launch_bounds__(1024) void group_one_kernel(const int32_t* __restri
     }
 }
 
-// out[t] = sum over the token's pairs of weight * y[pair], in the order of the pairs; y may be null (k = 1): only the
-// rows of tokens without a leaf are written, with zeros
+// out[t] = sum over the token's pairs of weight * y[pair], in the order of the pairs, V columns a thread
+template <int V>
 __global__ __launch_bounds__(256) void combine_kernel(const int32_t* __restrict__ idx, const float* __restrict__ weight, const float* __restrict__ y,
                                                       uint16_t* __restrict__ out, int64_t T, int64_t O, int64_t E, int k) {
-    const int64_t t = blockIdx.x;
-    if (!y) {
-        if ((uint32_t)idx[t] < E) return;
-        for (int64_t o = threadIdx.x; o < O; o += 256) out[t * O + o] = 0;
-        return;
-    }
-    for (int64_t o = threadIdx.x; o < O; o += 256) {
-        float v = 0;
-        for (int i = 0; i < k; ++i) {
-            if ((uint32_t)idx[t * k + i] >= E) continue;
-            v = fmaf(weight ? weight[t * k + i] : 1.0f, y[(t * k + i) * O + o], v);
+    const int64_t cols = O / V, id = (int64_t)blockIdx.x * 256 + threadIdx.x, t = id / cols, o = (id - t * cols) * V;
+    if (t >= T) return;
+    float v[V];
+#pragma unroll
+    for (int q = 0; q < V; ++q) v[q] = 0;
+#pragma unroll 4
+    for (int i = 0; i < k; ++i) {
+        const bool there = (uint32_t)idx[t * k + i] < E;
+        const float g = weight ? weight[t * k + i] : 1.0f;
+        float f[V];
+        if constexpr (V == 8) {
+            const float* const row = y + (t * k + i) * O + o;
+            widen<false>(*(const uint4*)row, f);
+            widen<false>(*(const uint4*)(row + 4), f + 4);
+        } else {
+            f[0] = y[(t * k + i) * O + o];
         }
-        out[t * O + o] = f32_to_bf16(v);
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] = there ? fmaf(g, f[q], v[q]) : v[q];
+    }
+    if constexpr (V == 8) *(uint4*)(out + t * O + o) = narrow<true>(v);
+    else out[t * O + o] = f32_to_bf16(v[0]);
+}
+
+// k = 1: the rows of tokens without a leaf
+__global__ __launch_bounds__(256) void clear_kernel(const int32_t* __restrict__ idx, uint16_t* __restrict__ out, int64_t T, int64_t O, int64_t E) {
+    for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < T; t += (int64_t)gridDim.x * 4) {
+        if ((uint32_t)idx[t] < E) continue;
+        for (int64_t o = threadIdx.x & 63; o < O; o += 64) out[t * O + o] = 0;
     }
 }
 
@@ -922,15 +982,11 @@ template <bool A4, int MODE> hipError_t launch_rows(const Args& a, int64_t tiles
     const int64_t blocks = (a.N + 15) / 16 * tiles;
     if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
     note_launch("mx4_rows_kernel<%s,%d,%s>", A4 ? "mx4" : "bf16", mt,
-                MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : MODE == kOutput ? "output" : MODE == kHiddenDirect ? "hidden,direct" : "output,direct");
+                MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : "output");
     const dim3 grid((unsigned)blocks);
-    if constexpr (MODE == kHiddenDirect || MODE == kOutputDirect) {
-        mx4_rows_kernel<A4, 1, MODE, 8><<<grid, 512, 0, s>>>(a);
-    } else {
-        if (mt == 1) mx4_rows_kernel<A4, 1, MODE, 8><<<grid, 512, 0, s>>>(a);
-        else if (mt == 2) mx4_rows_kernel<A4, 2, MODE, 8><<<grid, 512, 0, s>>>(a);
-        else mx4_rows_kernel<A4, 4, MODE, 4><<<grid, 256, 0, s>>>(a);
-    }
+    if (mt == 1) mx4_rows_kernel<A4, 1, MODE, 8><<<grid, 512, 0, s>>>(a);
+    else if (mt == 2) mx4_rows_kernel<A4, 2, MODE, 8><<<grid, 512, 0, s>>>(a);
+    else mx4_rows_kernel<A4, 4, MODE, 4><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -1039,8 +1095,8 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
         return hipGetLastError();
     }
     if (P <= 32) {
-        if ((e = launch_rows<false, kHiddenDirect>(a, P, 1, s)) != hipSuccess) return e;
-        return launch_rows<false, kOutputDirect>(b, p.T, 1, s);
+        if ((e = launch_direct<true>(a, P, s)) != hipSuccess) return e;
+        return launch_direct<false>(b, p.T, s);
     }
     const bool large = P / p.E >= 64;
     const int mt = rows_tile(P / p.E);
@@ -1079,8 +1135,17 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
         if ((e = launch_rows<false, kHidden>(a, tiles, mt, s)) != hipSuccess) return e;
         if ((e = launch_rows<false, kOutput>(b, tiles, mt, s)) != hipSuccess) return e;
     }
-    note_launch("combine_kernel");
-    combine_kernel<<<dim3((unsigned)p.T), 256, 0, s>>>(p.idx, p.weight, y, p.out, p.T, p.O, p.E, p.k);
+    if (!y) {
+        note_launch("clear_kernel");
+        clear_kernel<<<dim3((unsigned)(p.T < 4096 ? (p.T + 3) / 4 : 1024)), 256, 0, s>>>(p.idx, p.out, p.T, p.O, p.E);
+        return hipGetLastError();
+    }
+    const int v = p.O % 8 == 0 && ((uintptr_t)p.out & 15) == 0 ? 8 : 1;
+    const int64_t blocks = (p.T * (p.O / v) + 255) / 256;
+    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    note_launch("combine_kernel<%d>", v);
+    if (v == 8) combine_kernel<8><<<dim3((unsigned)blocks), 256, 0, s>>>(p.idx, p.weight, y, p.out, p.T, p.O, p.E, p.k);
+    else combine_kernel<1><<<dim3((unsigned)blocks), 256, 0, s>>>(p.idx, p.weight, y, p.out, p.T, p.O, p.E, p.k);
     return hipGetLastError();
 }
 

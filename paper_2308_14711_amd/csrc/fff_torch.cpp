@@ -12,6 +12,7 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 #include <c10/hip/HIPCachingAllocator.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include "../../include/fff.h"
@@ -86,6 +87,33 @@ struct Call {
             return 0;
         }
         return t->size(1);
+    }
+    // A tensor whose sizes the others' are derived from: dense, of one of these types, with `dims` sizes.
+    void* sized(int i, std::initializer_list<at::ScalarType> types, int dims, int64_t* sizes) {
+        const at::Tensor* t = tensor(i);
+        bool fits = t && t->dim() == dims && t->is_cuda() && t->is_contiguous();
+        if (fits) {
+            fits = false;
+            for (at::ScalarType k : types) fits = fits || t->scalar_type() == k;
+        }
+        if (!fits) {
+            ok = false;
+            for (int d = 0; d < dims; ++d) sizes[d] = 1;
+            return nullptr;
+        }
+        for (int d = 0; d < dims; ++d) sizes[d] = t->size(d);
+        return t->data_ptr();
+    }
+    // Every tensor so far lives on the current device, where the kernels and the scratch are.
+    void here(std::initializer_list<int> at) {
+        if (!ok) return;
+        const auto device = c10::hip::current_device();
+        for (int i : at)
+            if (args[i] != Py_None && THPVariable_Unpack(args[i]).get_device() != device) ok = false;
+    }
+    bool truth(int i) {
+        if (args[i] != Py_True && args[i] != Py_False) ok = false;
+        return args[i] == Py_True;
     }
     int code() const { return dtype == at::ScalarType::BFloat16 ? FFF_BF16 : FFF_F32; }
 };
@@ -249,6 +277,180 @@ PyObject* forward_block(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+constexpr at::ScalarType kF32 = at::ScalarType::Float, kBf16 = at::ScalarType::BFloat16, kI32 = at::ScalarType::Int, kU8 = at::ScalarType::Byte;
+constexpr std::initializer_list<at::ScalarType> kFloats = {kF32, kBf16};
+
+// a byte a token or none: uint8 or bool
+uint8_t* mask_of(Call& c, int i, int64_t T) {
+    const at::Tensor* t = c.tensor(i);
+    return (uint8_t*)c.dense(i, t && t->scalar_type() == at::ScalarType::Bool ? at::ScalarType::Bool : kU8, {T});
+}
+
+// logits, k, expert_idx, weight, count, prob_mean, loss, token_mask, normalise, stream
+PyObject* moe_route(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 10) return PyLong_FromLong(-1);
+    Call c{args};
+    int64_t size[2];
+    void* logits = c.sized(0, kFloats, 2, size);
+    const int64_t T = size[0], E = size[1];
+    if (c.ok) c.dtype = THPVariable_Unpack(args[0]).scalar_type();
+    const int k = c.integer(1, 1, 1 << 20);
+    int32_t* idx = (int32_t*)c.dense(2, kI32, {T, k});
+    float* weight = (float*)c.dense(3, kF32, {T, k});
+    int32_t* count = (int32_t*)c.dense(4, kI32, {E + 1});
+    float* mean = (float*)c.dense(5, kF32, {E});
+    float* loss = (float*)c.dense(6, kF32, {2});
+    uint8_t* mask = mask_of(c, 7, T);
+    const bool normalise = c.truth(8);
+    void* s = c.stream(9);
+    c.here({0, 2, 3, 4, 5, 6, 7});
+    return answer(c, [&] {
+        const auto call = [&](void* scratch, size_t bytes) {
+            return fff_moe_route(logits, mask, E, k, normalise, idx, weight, count, mean, loss, s, T, c.code(), scratch, bytes);
+        };
+        const size_t bytes = count || mean || loss ? fff_route_scratch_bytes(T, E) : 0;
+        if (bytes == 0) return call(nullptr, 0);
+        if (captured(s)) return -1;
+        const Scratch scratch(bytes, (hipStream_t)s);
+        return scratch.p ? call(scratch.p, bytes) : -1;
+    });
+}
+
+// logits, expert_idx, count, dlogits, dweight, dloss, token_mask, normalise, stream
+PyObject* moe_route_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 9) return PyLong_FromLong(-1);
+    Call c{args};
+    int64_t size[2], slots[2];
+    void* logits = c.sized(0, kFloats, 2, size);
+    const int64_t T = size[0], E = size[1];
+    if (c.ok) c.dtype = THPVariable_Unpack(args[0]).scalar_type();
+    int32_t* idx = (int32_t*)c.sized(1, {kI32}, 2, slots);
+    c.ok = c.ok && slots[0] == T && slots[1] <= 1 << 20;
+    int32_t* count = (int32_t*)c.dense(2, kI32, {E + 1});
+    void* dlogits = c.need(3, {T, E});
+    float* dweight = (float*)c.dense(4, kF32, {T, slots[1]});
+    float* dloss = (float*)c.dense(5, kF32, {2});
+    uint8_t* mask = mask_of(c, 6, T);
+    const bool normalise = c.truth(7);
+    void* s = c.stream(8);
+    c.here({0, 1, 2, 3, 4, 5, 6});
+    return answer(c, [&] {
+        return fff_moe_route_backward(logits, mask, E, (int)slots[1], normalise, idx, count, dweight, dloss, dlogits, s, T, c.code());
+    });
+}
+
+int64_t mx4_blocks(int64_t n) { return (n + 31) / 32; }
+
+// src, codes, scales, transpose, stream
+PyObject* mx4_quantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 5) return PyLong_FromLong(-1);
+    Call c{args};
+    int64_t size[3] = {1, 1, 1};
+    const at::Tensor* src = c.tensor(0);
+    const bool batched = src && src->dim() == 3;
+    void* p = c.sized(0, kFloats, batched ? 3 : 2, batched ? size : size + 1);
+    if (c.ok) c.dtype = src->scalar_type();
+    const bool transpose = c.truth(3);
+    const int64_t rows = transpose ? size[2] : size[1], blocks = mx4_blocks(transpose ? size[1] : size[2]);
+    uint8_t *codes, *scales;
+    if (batched) {
+        codes = (uint8_t*)c.dense(1, kU8, {size[0], rows, 16 * blocks});
+        scales = (uint8_t*)c.dense(2, kU8, {size[0], rows, blocks});
+    } else {
+        codes = (uint8_t*)c.dense(1, kU8, {rows, 16 * blocks});
+        scales = (uint8_t*)c.dense(2, kU8, {rows, blocks});
+    }
+    void* s = c.stream(4);
+    c.here({0, 1, 2});
+    return answer(c, [&] { return fff_mx4_quantize(p, codes, scales, transpose, s, size[0], size[1], size[2], c.code()); });
+}
+
+// codes, scales, out, stream
+PyObject* mx4_dequantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 4) return PyLong_FromLong(-1);
+    Call c{args};
+    int64_t size[3] = {1, 1, 1};
+    const at::Tensor* out = c.tensor(2);
+    const bool batched = out && out->dim() == 3;
+    void* p = c.sized(2, kFloats, batched ? 3 : 2, batched ? size : size + 1);
+    if (c.ok) c.dtype = out->scalar_type();
+    const int64_t blocks = mx4_blocks(size[2]);
+    uint8_t *codes, *scales;
+    if (batched) {
+        codes = (uint8_t*)c.dense(0, kU8, {size[0], size[1], 16 * blocks});
+        scales = (uint8_t*)c.dense(1, kU8, {size[0], size[1], blocks});
+    } else {
+        codes = (uint8_t*)c.dense(0, kU8, {size[1], 16 * blocks});
+        scales = (uint8_t*)c.dense(1, kU8, {size[1], blocks});
+    }
+    void* s = c.stream(3);
+    c.here({0, 1, 2});
+    return answer(c, [&] { return fff_mx4_dequantize(codes, scales, p, s, size[0] * size[1], size[2], c.code()); });
+}
+
+// a, w_codes, w_scales, out, a_scales, bias, act, stream
+PyObject* mx4_product(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 8) return PyLong_FromLong(-1);
+    Call c{args};
+    int64_t a_size[2], out_size[2], blocks[2] = {0, 0};
+    const bool codes = args[4] != Py_None;
+    void* a = c.sized(0, {codes ? kU8 : kBf16}, 2, a_size);
+    void* out = c.sized(3, kFloats, 2, out_size);
+    if (c.ok) c.dtype = THPVariable_Unpack(args[3]).scalar_type();
+    const int64_t T = out_size[0], N = out_size[1];
+    uint8_t* a_scales = codes ? (uint8_t*)c.sized(4, {kU8}, 2, blocks) : nullptr;
+    const int64_t Kb = codes ? blocks[1] : mx4_blocks(a_size[1]), K = codes ? 32 * Kb : a_size[1];
+    c.ok = c.ok && a_size[0] == T && (!codes || (blocks[0] == T && a_size[1] == 16 * Kb));
+    uint8_t* w = (uint8_t*)c.dense(1, kU8, {N, 16 * Kb});
+    uint8_t* w_scales = (uint8_t*)c.dense(2, kU8, {N, Kb});
+    void* bias = c.dense(5, c.dtype, {N});
+    const int act = c.integer(6, 0, 2);
+    void* s = c.stream(7);
+    c.here({0, 1, 2, 3, 4, 5});
+    return answer(c, [&] {
+        const auto call = [&](void* scratch, size_t bytes) {
+            return fff_mx4_product(a, a_scales, w, w_scales, bias, act, out, s, T, K, N, c.code(), scratch, bytes);
+        };
+        const bool copies = !codes && (K % 8 != 0 || ((uintptr_t)a & 15) != 0);
+        const size_t bytes = copies ? fff_mx4_product_scratch_bytes(T, K) : 0;
+        if (bytes == 0) return call(nullptr, 0);
+        if (captured(s)) return -1;
+        const Scratch scratch(bytes, (hipStream_t)s);
+        return scratch.p ? call(scratch.p, bytes) : -1;
+    });
+}
+
+// x, leaf_w1, leaf_s1, leaf_b1, leaf_w2, leaf_s2, leaf_b2, leaf_idx, weight, act, out, stream
+PyObject* leaf_forward_mx4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 12) return PyLong_FromLong(-1);
+    Call c{args};
+    int64_t x_size[2], out_size[2], b1_size[2], idx_size[2] = {1, 1};
+    void* x = c.sized(0, {kBf16}, 2, x_size);
+    void* out = c.sized(10, {kBf16}, 2, out_size);
+    void* b1 = c.sized(3, {kBf16}, 2, b1_size);
+    const at::Tensor* ids = c.tensor(7);
+    const bool vector = ids && ids->dim() == 1;
+    int32_t* idx = (int32_t*)c.sized(7, {kI32}, vector ? 1 : 2, idx_size);
+    const int64_t T = x_size[0], D = x_size[1], O = out_size[1], E = b1_size[0], L = b1_size[1], k = idx_size[1];
+    c.ok = c.ok && out_size[0] == T && idx_size[0] == T && k <= 1 << 20 && L <= 1 << 20;
+    uint8_t* w1 = (uint8_t*)c.dense(1, kU8, {E, L, 16 * mx4_blocks(D)});
+    uint8_t* s1 = (uint8_t*)c.dense(2, kU8, {E, L, mx4_blocks(D)});
+    uint8_t* w2 = (uint8_t*)c.dense(4, kU8, {E, O, 16 * mx4_blocks(L)});
+    uint8_t* s2 = (uint8_t*)c.dense(5, kU8, {E, O, mx4_blocks(L)});
+    void* b2 = c.dense(6, kBf16, {E, O});
+    float* weight = (float*)(vector ? c.dense(8, kF32, {T}) : c.dense(8, kF32, {T, k}));
+    const int act = c.integer(9, 0, 1);
+    void* s = c.stream(11);
+    c.here({0, 1, 2, 3, 4, 5, 6, 7, 8, 10});
+    return answer(c, [&] {
+        const size_t bytes = fff_leaf_mx4_scratch_bytes(T, D, O, E, (int)k, (int)L);
+        if (bytes == 0 || captured(s)) return -1;
+        const Scratch scratch(bytes, (hipStream_t)s);
+        if (!scratch.p) return -1;
+        return fff_leaf_forward_mx4(x, w1, s1, b1, w2, s2, b2, idx, weight, E, (int)k, (int)L, act, out, s, T, D, O, FFF_BF16, scratch.p, bytes);
+    });
+}
+
 // torch's accessors may throw (a tensor without storage, no device): not an ordinary call either
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -261,7 +463,8 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 
 #define FFF_METHOD(f) {#f, (PyCFunction)(void (*)(void))guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FFF_METHOD(forward_hard), FFF_METHOD(moe_top1_forward), FFF_METHOD(forward_soft),
-                         FFF_METHOD(forward_block), {nullptr, nullptr, 0, nullptr}};
+                         FFF_METHOD(forward_block), FFF_METHOD(moe_route), FFF_METHOD(moe_route_backward), FFF_METHOD(mx4_quantize),
+                         FFF_METHOD(mx4_dequantize), FFF_METHOD(mx4_product), FFF_METHOD(leaf_forward_mx4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fff_torch", "Native calls of binding.py", -1, methods};
 
 }  // namespace
