@@ -20,6 +20,10 @@ __device__ __forceinline__ const char* uniform(const char* p) {
     const uint64_t v = (uint64_t)p;
     return (const char*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32);
 }
+// four bytes a lane straight to LDS: lane i's land at lds + 4 i
+__device__ __forceinline__ void load_word_to_lds(const char* src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory");
+}
 // load_to_lds from a base that the wave shares
 __device__ __forceinline__ void load_to_lds_from(const char* base, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
@@ -301,10 +305,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
 // are converted once a block).  A stage is 64 elements of K (bf16 rows: 128 bytes of a row of A, 32 of W) or 128 (codes: 64 bytes of either); of the
 // three stages in LDS one is multiplied and two are on their way, straight from memory.  Two blocks share a compute unit, and one multiplies while the
 // other waits or ends.  (4096 x 4096 x 4096 and 16384 x 2048 x 768 of bf16 rows, 8192 x 4096 x 4096 of codes: 134, 59 and 117 us; a wave on 64 x 64: 145,
-// 61, 131; eight waves on 256 x 256, half of them reading while the others multiply: 138, 65, 134.)
-// The scale bytes of 128 blocks of every row (4096 elements of K) are put into LDS at once: a row's scales of one stage are a few bytes in a line of
-// their own, so that fetching them stage by stage cost as much as the codes (8192 x 4096 x 4096, four bits both: 121 us without such
-// loads, 174 with them).
+// 61, 131; eight waves on 256 x 256, half of them reading while the others multiply: 138, 65, 134; all three before the panels below.)
+// Scale bytes come in panels of 32 blocks (1024 elements of K) of every row, with the first stage that they belong to: a row's scales of one stage are
+// a few bytes in a line of their own, so that fetching them stage by stage cost as much as the codes (8192 x 4096 x 4096, four bits both: 121 us without
+// such loads, 174 with them), and a panel of the whole K before the first stage was a third of a short K's time (16384 x 768 x 2048: 87 -> 71 us).
 //
 // Lane (j, g) multiplies, of a stage of bf16 rows, elements 16 g + 8 u .. + 7 in step u (pieces 2 g + u of A, four bytes of codes); of a stage of codes,
 // block g.  Pieces of 16 bytes in LDS are turned within their row so that the 16 lanes of a pass of an operand read (rows
@@ -312,16 +316,13 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
 // the lanes' source addresses, since a load to LDS writes lane after lane: 128-byte rows as tile_swz, 64-byte rows by 2 (row >> 3 & 1), 32-byte rows
 // (read eight bytes a lane) not at all.
 __device__ const uint4 g_zero_piece = {0, 0, 0, 0};
-constexpr int kPanel = 128;      // blocks whose scales are in LDS
+constexpr int kPanel = 32;       // blocks whose scales come together
 
 template <int ROW> __device__ __forceinline__ int turn(int row) { return ROW == 128 ? lds_rot(row) : ROW == 64 ? 2 * ((row >> 3) & 1) : 0; }
 template <int ROW> __device__ __forceinline__ int lds_slot(int row, int piece) {
     constexpr int n = ROW / 16;
     return row * n + ((piece + turn<ROW>(row)) & (n - 1));
 }
-// byte of block b (of the panel) of a row: pieces of 16 exchanged so that eight rows' lie in different banks
-__device__ __forceinline__ int scale_slot(int row, int b) { return row * kPanel + (b ^ ((row & 7) << 4)); }
-
 template <bool A4, int MT> struct TileShape {
     static constexpr int kThreads = 256, kWaves = 4, NT = 2, kRows = 16 * MT, kCols = 128;
     static constexpr int kARow = A4 ? 64 : 128, kWRow = A4 ? 64 : 32;           // bytes of a row in a stage
@@ -329,23 +330,23 @@ template <bool A4, int MT> struct TileShape {
     static constexpr int kABytes = kRows * kARow, kWBytes = kCols * kWRow, kStage = kABytes + kWBytes;
     static constexpr int kALoads = kABytes / 1024 / kWaves, kWLoads = kWBytes / 1024 / kWaves;   // a wave's loads of 1 KB a stage
     static_assert(kALoads * 1024 * kWaves == kABytes && kWLoads * 1024 * kWaves == kWBytes, "whole loads a wave");
-    static constexpr int kScaleRows = kCols + (A4 ? kRows : 0);
-    static constexpr int kLds = 3 * kStage + kScaleRows * kPanel;
+    static constexpr int kScaleRows = kCols + (A4 ? 128 : 0);      // (rows behind the last: its scales again)
+    static constexpr int kPanelBytes = kScaleRows * kPanel, kPanelStages = kPanel / kStageBlocks, kPanelLoads = kPanelBytes / 1024 / kWaves, kPanelWords = kPanelBytes / 256 / kWaves;
+    static constexpr int kLds = 3 * kStage + 2 * kPanelBytes;
 };
 
 template <bool A4, int MODE, bool WIDE, int MT>
-__global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const int64_t row_tiles, const int64_t col_tiles) {
+__global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const uint32_t row_tiles, const uint32_t col_tiles) {
     typedef TileShape<A4, MT> S;
     constexpr int NT = S::NT;
     extern __shared__ __align__(16) char lds[];
-    uint8_t* const scales = (uint8_t*)lds + 3 * S::kStage;
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
     // an XCD takes a contiguous range of tiles, kGroup row tiles against all columns at a time
-    constexpr int kGroup = 4;
-    const int64_t id = xcd_contiguous_block();
+    constexpr uint32_t kGroup = 4;
+    const uint32_t id = (blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;
     if (id >= row_tiles * col_tiles) return;
-    const int64_t group = id / (kGroup * col_tiles), in = id - group * kGroup * col_tiles;
-    const int64_t tall = row_tiles - kGroup * group < kGroup ? row_tiles - kGroup * group : kGroup;
+    const uint32_t group = id / (kGroup * col_tiles), in = id - group * kGroup * col_tiles;
+    const uint32_t tall = row_tiles - kGroup * group < kGroup ? row_tiles - kGroup * group : kGroup;
     const int64_t rt = kGroup * group + in % tall, ct = in / tall;
     const int64_t n0 = ct * S::kCols;
     int64_t leaf = 0, first, rows;
@@ -397,7 +398,44 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const in
     const int a_pieces = A4 ? a.Kb : a.pieces;
     const int whole = a_pieces / (S::kARow / 16) < a.Kb / S::kStageBlocks ? a_pieces / (S::kARow / 16) : a.Kb / S::kStageBlocks;
     const uint32_t lds0 = lds_address(lds) + wv * 1024;
+    // Scales of a panel of all rows, zeros behind a row's end (zero codes times 2^-127): straight to LDS, 16 bytes a lane where rows of scales are whole
+    // aligned pieces, else four, or through registers where they are not even that.
+    const uintptr_t scale_bits = (uintptr_t)a.w_scales | (A4 ? (uintptr_t)a.a_scales : 0) | (uintptr_t)a.Kb;
+    const int scale_width = scale_bits % 16 == 0 ? 16 : scale_bits % 4 == 0 ? 4 : 1;
+    const auto scales_of = [&](int row) { return row < S::kCols ? a.w_scales + w_index(row) * a.Kb : a.a_scales + a_index(row - S::kCols) * a.Kb; };
+    const char* s_src[S::kPanelLoads];
+#pragma unroll
+    for (int i = 0; i < S::kPanelLoads; ++i) s_src[i] = (const char*)scales_of((i * S::kWaves + wv) * 32 + lane / 2) + 16 * (lane % 2);
+    const auto fetch_panel = [&](int panel) {
+        const int b0 = panel * kPanel, to = 3 * S::kStage + (panel & 1) * S::kPanelBytes;
+        if (scale_width == 16) {
+#pragma unroll
+            for (int i = 0; i < S::kPanelLoads; ++i)
+                load_to_lds(b0 + 16 * (lane % 2) < a.Kb ? s_src[i] + b0 : (const char*)&g_zero_piece,
+                            __builtin_amdgcn_readfirstlane(lds_address(lds) + to + (i * S::kWaves + wv) * 1024));
+            return;
+        }
+        if (scale_width == 4) {
+#pragma unroll 1
+            for (int i = 0; i < S::kPanelWords; ++i) {
+                const int first = (i * S::kWaves + wv) * 64, at = first + lane, b = b0 + 4 * (at % 8);
+                load_word_to_lds(b < a.Kb ? (const char*)scales_of(at / 8) + b : (const char*)&g_zero_piece,
+                                 __builtin_amdgcn_readfirstlane(lds_address(lds) + to + 4 * first));
+            }
+            return;
+        }
+#pragma unroll 1
+        for (int at = tid; at < S::kScaleRows * 8; at += S::kThreads) {
+            const int b = b0 + 4 * (at % 8);
+            const uint8_t* const src = scales_of(at / 8) + b;
+            uint32_t q = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q |= (uint32_t)(b + e < a.Kb ? src : (const uint8_t*)&g_zero_piece)[e] << (8 * e);
+            *(uint32_t*)(lds + to + 4 * at) = q;
+        }
+    };
     const auto fetch = [&](int c, int buf) {
+        if (c % S::kPanelStages == 0) fetch_panel(c / S::kPanelStages);
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + buf * S::kStage);
         const char* const as = a_base + (int64_t)c * S::kARow;
         const char* const ws = w_base + (int64_t)c * S::kWRow;
@@ -419,48 +457,6 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const in
                 load_to_lds(c * (S::kWRow / 16) + w_piece(i) < a.Kb ? ws + w_off[i] : zero, at + S::kABytes + i * S::kWaves * 1024);
         }
     };
-    // Scales of blocks b0 .. b0 + 127 of all rows, zeros behind a row's end (zero codes times 2^-127): straight to LDS where rows of scales are whole
-    // aligned pieces, else through registers, BATCH loads at once (one where the accumulators are live).
-    const bool scales_aligned = a.Kb % 16 == 0 && (((uintptr_t)a.w_scales | (A4 ? (uintptr_t)a.a_scales : 0)) & 15) == 0;
-    const auto scales_of = [&](int row) { return row < S::kCols ? a.w_scales + w_index(row) * a.Kb : a.a_scales + a_index(row - S::kCols) * a.Kb; };
-    const auto fetch_scales = [&](int b0, auto BATCH) {
-        constexpr int kPieces = kPanel / 16, kAll = S::kScaleRows * kPieces, kBatch = decltype(BATCH)::value;
-        static_assert(kAll % (kBatch * S::kThreads) == 0 && kPieces == 8, "");
-        if (scales_aligned) {
-#pragma unroll 1
-            for (int i0 = 64 * wv; i0 < kAll; i0 += S::kThreads) {
-                const int i = i0 + lane, row = i / kPieces, b = b0 + 16 * ((i % kPieces) ^ (row & 7));      // (the piece that scale_slot puts here)
-                load_to_lds(b < a.Kb ? (const char*)scales_of(row) + b : (const char*)&g_zero_piece,
-                            __builtin_amdgcn_readfirstlane(lds_address(scales) + 16 * i0));
-            }
-            wait_loads<0>();
-            return;
-        }
-#pragma unroll 1
-        for (int i0 = tid; i0 < kAll; i0 += kBatch * S::kThreads) {
-            uint4 v[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int i = i0 + u * S::kThreads, b = b0 + 16 * (i % kPieces);
-                v[u] = load_bytes(b + 16 <= a.Kb ? scales_of(i / kPieces) + b : (const uint8_t*)&g_zero_piece);
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int i = i0 + u * S::kThreads, b = b0 + 16 * (i % kPieces);
-                if (b < a.Kb && b + 16 > a.Kb) {
-                    const uint8_t* const src = scales_of(i / kPieces) + b;
-                    uint32_t q[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (b + e < a.Kb) q[e / 4] |= (uint32_t)src[e] << (8 * (e % 4));
-                    v[u] = make_uint4(q[0], q[1], q[2], q[3]);
-                }
-                *(uint4*)(scales + scale_slot(i / kPieces, 16 * (i % kPieces))) = v[u];
-            }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    };
-
     f32x4_t acc[NT][MT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -473,7 +469,8 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const in
     const auto read = [&](int c, int buf) {
         const uint4* const la = (const uint4*)(lds + buf * S::kStage);
         const char* const lw = lds + buf * S::kStage + S::kABytes;
-        const int b0 = c * S::kStageBlocks % kPanel, b = b0 + (A4 ? g : g >> 1);
+        const uint8_t* const scales = (const uint8_t*)lds + 3 * S::kStage + (c / S::kPanelStages & 1) * S::kPanelBytes + c * S::kStageBlocks % kPanel;
+        const int b = A4 ? g : g >> 1;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int row = 16 * (wv * NT + n) + j;
@@ -484,14 +481,14 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const in
                 fw[n].x = v.x;
                 fw[n].y = v.y;
             }
-            ws[n] = scales[scale_slot(row, b)];
+            ws[n] = scales[row * kPanel + b];
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int row = 16 * m + j;
 #pragma unroll
             for (int u = 0; u < kSteps; ++u) fa[u][m] = la[A4 ? lds_slot<64>(row, g) : lds_slot<128>(row, 2 * g + u)];
-            if constexpr (A4) as[m] = scales[scale_slot(S::kCols + row, b0 + g)];
+            if constexpr (A4) as[m] = scales[(S::kCols + row) * kPanel + b];
         }
     };
     const auto multiply = [&]() {
@@ -515,28 +512,30 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const in
         asm volatile("s_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    fetch(0, 0);
-    if (stages > 1) fetch(1, 1);
-    if (stages > 2) fetch(2, 2);
-    fetch_scales(0, std::integral_constant<int, 2>());
-    wait_loads<0>();
-    __syncthreads();
+    // (the epilogue's: asked for here, where the wait for them is the stages')
+    constexpr int kLanes = 2 * NT;
+    const int64_t n8 = n0 + 16 * NT * wv + 8 * (lane % kLanes);
+    float bias[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        bias[q] = n8 + q >= a.N ? 0.f : MODE == kDense ? bias_at(a, a.bias, n8 + q) : bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n8 + q]);
+#pragma unroll 1
+    for (int c = 0; c < 3 && c < stages; ++c) fetch(c, c);
+    if (stages > 2) wait_loads<2 * kLoads>();
+    else wait_loads<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
     int buf = 0;
-    // Everybody has read stage c: its buffer takes stage c + 3, and at the end of a panel of scales the next one comes.
-    const auto turn_over = [&](int c) {
-        if (c + 3 < stages) fetch(c + 3, buf);
-        if ((c + 1) * S::kStageBlocks % kPanel == 0 && c + 1 < stages) {
-            fetch_scales((c + 1) * S::kStageBlocks, std::integral_constant<int, 1>());
-            barrier();
-        }
-    };
     for (int c = 0; c < stages; ++c) {
         read(c, buf);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (c + 2 < stages) wait_loads<kLoads>();      // this wave's part of stage c + 1 is there
-        else wait_loads<0>();
+        // this wave's part of stage c + 1 is there (stage c + 2 may be on its way, with a panel of scales or without)
+        if (c + 2 >= stages) wait_loads<0>();
+        else if ((c + 2) % S::kPanelStages != 0 || scale_width == 1) wait_loads<kLoads>();
+        else if (scale_width == 16) wait_loads<kLoads + S::kPanelLoads>();
+        else wait_loads<kLoads + S::kPanelWords>();
         barrier();
-        turn_over(c);
+        if (c + 3 < stages) fetch(c + 3, buf);      // (everybody has read stage c)
         multiply();
         buf = buf == 2 ? 0 : buf + 1;
     }
@@ -544,15 +543,10 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const in
     // Results through LDS, half of the wave's rows at a time, so that they leave as whole rows of 16 NT columns, eight a lane, from a loop:
     // written out for every accumulator the epilogue was more code than the instruction cache takes, and fetching it took longer than
     // the stages of a short K.
-    constexpr int kHalf = MT / 2, kPitch = 16 * NT + 4, kLanes = 2 * NT, kRowsAtOnce = 64 / kLanes;
+    constexpr int kHalf = MT / 2, kPitch = 16 * NT + 4, kRowsAtOnce = 64 / kLanes;
     static_assert(S::kWaves * 16 * kHalf * kPitch * 4 <= S::kLds, "results fit where the stages were");
     float* const part = (float*)lds + wv * 16 * kHalf * kPitch;
     const int64_t limit = MODE == kHidden ? a.out_row : a.N;
-    const int64_t n8 = n0 + 16 * NT * wv + 8 * (lane % kLanes);
-    float bias[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-        bias[q] = n8 + q >= a.N ? 0.f : MODE == kDense ? bias_at(a, a.bias, n8 + q) : bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n8 + q]);
     __syncthreads();
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -597,7 +591,7 @@ template <bool A4, int MODE, int MT> hipError_t launch_tiles(Args a, int64_t row
     const auto kernel = wide ? mx4_tile_kernel<A4, MODE, MODE == kHidden, MT> : mx4_tile_kernel<A4, MODE, false, MT>;
     const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
     if (e != hipSuccess) return e;
-    kernel<<<dim3((unsigned)blocks), S::kThreads, S::kLds, s>>>(a, row_tiles, col_tiles);
+    kernel<<<dim3((unsigned)blocks), S::kThreads, S::kLds, s>>>(a, (uint32_t)row_tiles, (uint32_t)col_tiles);
     return hipGetLastError();
 }
 
