@@ -84,31 +84,52 @@ template <bool BF16, bool VEC> __device__ __forceinline__ int element(int v, int
     return VEC ? (v / VE * G + gi) * VE + v % VE : v * G + gi;
 }
 
-template <bool BF16, int V, bool VEC> __device__ __forceinline__ void load_row(const RouteArgs& a, int64_t t, int gi, float (&l)[V]) {
-    constexpr int VE = BF16 ? 8 : 4, es = BF16 ? 2 : 4;
-    const char* const row = (const char*)a.logits + t * a.E * es;
-    const float ninf = -__builtin_inff();
-    if (VEC) {
+// A row as it lies in memory, asked for ahead of its use.
+template <bool BF16, int V, bool VEC> struct RawRow {
+    static constexpr int VE = BF16 ? 8 : 4, es = BF16 ? 2 : 4;
+    uint4 q[VEC ? V / VE : 1];
+    typename Elem<BF16>::type x[VEC ? 1 : V];
+    uint8_t on;
+    __device__ __forceinline__ void load(const RouteArgs& a, int64_t t, int gi) {
+        t = t < a.T ? t : a.T - 1;
+        const char* const row = (const char*)a.logits + t * a.E * es;
+        on = a.mask ? a.mask[t] : 1;
+        if constexpr (VEC) {
 #pragma unroll
-        for (int v = 0; v < V; v += VE) {
-            const int e = element<BF16, VEC>(v, gi, a.lanes);
-            const uint4 q = *(const uint4*)(row + (e < a.E ? e : 0) * es);
-            widen<BF16>(q, l + v);
+            for (int v = 0; v < V; v += VE) {
+                const int e = element<BF16, VEC>(v, gi, a.lanes);
+                q[v / VE] = *(const uint4*)(row + (e < a.E ? e : 0) * es);
+            }
+        } else {
 #pragma unroll
-            for (int i = 0; i < VE; ++i)
-                if (e >= a.E) l[v + i] = ninf;
-        }
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = element<BF16, VEC>(v, gi, a.lanes);
-            l[v] = Elem<BF16>::load(row, e < a.E ? e : 0);
-            if (e >= a.E) l[v] = ninf;
+            for (int v = 0; v < V; ++v) {
+                const int e = element<BF16, VEC>(v, gi, a.lanes);
+                x[v] = ((const typename Elem<BF16>::type*)row)[e < a.E ? e : 0];
+            }
         }
     }
+    // its logits: -infinity for NaN, behind the row's end and in a row that takes no part; whether there are others
+    __device__ __forceinline__ bool values(const RouteArgs& a, bool there, int gi, float (&l)[V], float* largest) const {
+        const float ninf = -__builtin_inff();
+        if constexpr (VEC) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) l[v] = l[v] != l[v] ? ninf : l[v];
-}
+            for (int v = 0; v < V; v += VE) widen<BF16>(q[v / VE], l + v);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) l[v] = Elem<BF16>::load(x, v);
+        }
+        float m = ninf;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const bool in = there && on && element<BF16, VEC>(v, gi, a.lanes) < a.E;
+            l[v] = in && l[v] == l[v] ? l[v] : ninf;
+            m = fmaxf(m, l[v]);
+        }
+        m = group_max(m, a.lanes);
+        *largest = m;
+        return m > ninf;
+    }
+};
 
 // exp(l - m) for l <= m, m > -infinity; logits of +infinity share the row.  The product with log2(e) is carried in two parts: rounded to
 // one, it would leave a relative error of up to 2^-19 where l lies far below m.
@@ -210,7 +231,6 @@ __global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteA
     int32_t* const my_i = (int32_t*)lds + slots + (tid / G) * k;
     float* const sums = lds + 2 * slots;
     int32_t* const counts = (int32_t*)sums + kWaves * E;
-    const float ninf = -__builtin_inff();
     float acc[V], z = 0;
     int n = 0;
 #pragma unroll
@@ -220,20 +240,16 @@ __global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteA
         __syncthreads();
     }
     const int64_t step = (int64_t)gridDim.x * kWaves * rows;
+    int64_t t0 = ((int64_t)blockIdx.x * kWaves + wv) * rows;
+    RawRow<BF16, V, VEC> raw;
+    if (t0 < a.T) raw.load(a, t0 + lane / G, gi);
     // (rows past the end and masked ones run along as empty rows: the lanes of a wave stay together)
-    for (int64_t t0 = ((int64_t)blockIdx.x * kWaves + wv) * rows; t0 < a.T; t0 += step) {
+    for (; t0 < a.T; t0 += step) {
         const int64_t t = t0 + lane / G;
-        const bool there = t < a.T, on = there && (!a.mask || a.mask[t]);
-        float l[V];
-        load_row<BF16, V, VEC>(a, there ? t : a.T - 1, gi, l);
-        float m = ninf;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (!on) l[v] = ninf;
-            m = fmaxf(m, l[v]);
-        }
-        m = group_max(m, G);
-        const bool any = m > ninf;
+        const bool there = t < a.T;
+        float l[V], m;
+        const bool any = raw.values(a, there, gi, l, &m);
+        if (t0 + step < a.T) raw.load(a, t + step, gi);
         float total = 0;
         if (stats || !a.normalise) {
             float p[V];
@@ -401,7 +417,6 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
     constexpr int VE = BF16 ? 8 : 4, es = BF16 ? 2 : 4;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int G = a.lanes, gi = lane & (G - 1), rows = 64 / G, E = a.E, k = a.k;
-    const float ninf = -__builtin_inff();
     float* const patch = patches + (tid / G) * (G * V);
     for (int i = lane; i < 64 * V; i += 64) patches[wv * 64 * V + i] = 0;
     wave_sync();
@@ -421,20 +436,34 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
         }
     }
     const int64_t step = (int64_t)gridDim.x * kBackwardWaves * rows;
+    // slots of a row that this lane looks after: gi, gi + G, ... (k <= E <= G V, and k <= 32)
+    constexpr int kSlots = V == 8 ? 8 : 1;
     for (int64_t t0 = ((int64_t)blockIdx.x * kBackwardWaves + wv) * rows; t0 < a.T; t0 += step) {
         const int64_t t = t0 + lane / G;
-        const bool there = t < a.T, on = there && (!a.mask || a.mask[t]);
+        const bool there = t < a.T;
         const int64_t tt = there ? t : a.T - 1;
-        float l[V], d[V];
-        load_row<BF16, V, VEC>(a, tt, gi, l);
-        float m = ninf;
+        const char* const row = (const char*)a.logits + tt * E * es;
+        RawRow<BF16, V, VEC> raw;
+        raw.load(a, t, gi);
+        // everything else that the row needs from memory is asked for before the first wait
+        uint32_t slot_e[kSlots];
+        float slot_g[kSlots], slot_x[kSlots];
+        if (a.dweight) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (!on) l[v] = ninf;
-            m = fmaxf(m, l[v]);
+            for (int s = 0; s < kSlots; ++s) {
+                if (s * G >= k) break;
+                const int i = gi + s * G;
+                slot_e[s] = i < k ? (uint32_t)a.idx[tt * k + i] : ~0u;
+                slot_g[s] = i < k ? a.dweight[tt * k + i] : 0.0f;
+            }
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s) {
+                if (s * G >= k) break;
+                slot_x[s] = Elem<BF16>::load(row, slot_e[s] < (uint32_t)E ? slot_e[s] : 0);
+            }
         }
-        m = group_max(m, G);
-        const bool any = m > ninf;
+        float l[V], d[V], m;
+        const bool any = raw.values(a, there, gi, l, &m);
         float s = 0, dot = 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -451,15 +480,15 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
         for (int v = 0; v < V; ++v) d[v] = l[v] > 0.0f ? l[v] * inv * (pull[v] - dot + zz) : 0.0f;
         if (a.dweight) {
             // The slots' part: a lane a slot, put to where the expert's lane reads it.  (Rows that take no part run along.)
-            const char* const row = (const char*)a.logits + tt * E * es;
             float sum = 0, mean = 0;
-            for (int i = gi; i < k; i += G) {
-                const uint32_t e = any ? (uint32_t)a.idx[tt * k + i] : ~0u;
-                if (e >= (uint32_t)E) continue;
-                const float x = Elem<BF16>::load(row, e);
-                const float w = x == x ? relative(x, m) : 0.0f;
-                sum += w;
-                mean = fmaf(w, a.dweight[tt * k + i], mean);
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s) {
+                if (s * G >= k) break;
+                const bool good = any && slot_e[s] < (uint32_t)E && slot_x[s] == slot_x[s];
+                slot_x[s] = good ? relative(slot_x[s], m) : 0.0f;
+                slot_g[s] = any && slot_e[s] < (uint32_t)E ? slot_g[s] : 0.0f;         // (no expert's: not read)
+                sum += slot_x[s];
+                mean = fmaf(slot_x[s], slot_g[s], mean);
             }
             sum = group_add(sum, G);
             mean = group_add(mean, G);
@@ -469,20 +498,19 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
 #pragma unroll
                 for (int v = 0; v < V; ++v) d[v] = fmaf(-l[v] * inv, mean, d[v]);
             }
-            for (int i = gi; i < k; i += G) {
-                const uint32_t e = any ? (uint32_t)a.idx[tt * k + i] : ~0u;
-                if (e >= (uint32_t)E) continue;
-                const float x = Elem<BF16>::load(row, e);
-                const float w = x == x ? relative(x, m) : 0.0f;
-                atomicAdd(patch + e, w * by * (a.dweight[tt * k + i] - (a.normalise ? mean : 0.0f)));
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s) {
+                if (s * G >= k) break;
+                if (any && slot_e[s] < (uint32_t)E) atomicAdd(patch + slot_e[s], slot_x[s] * by * (slot_g[s] - (a.normalise ? mean : 0.0f)));
             }
             wave_sync();
 #pragma unroll
             for (int v = 0; v < V; ++v) d[v] += patch[element<BF16, VEC>(v, gi, G)];
             wave_sync();
-            for (int i = gi; i < k; i += G) {
-                const uint32_t e = any ? (uint32_t)a.idx[tt * k + i] : ~0u;
-                if (e < (uint32_t)E) patch[e] = 0;
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s) {
+                if (s * G >= k) break;
+                if (slot_e[s] < (uint32_t)E) patch[slot_e[s]] = 0;
             }
             wave_sync();
         }

@@ -88,9 +88,12 @@ __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const char* _
     const int64_t r0 = at / col_tiles * kTransRows, c0 = at % col_tiles * kTransCols;
     src += b * rows * cols * es;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    // (addresses of elements behind the matrix: its first; sixteen loads a wave on their way at once)
+#pragma unroll 16
     for (int r = wv; r < kTransRows; r += 4) {
         const bool in = r0 + r < rows && c0 + lane < cols;
-        tile[r][lane] = in ? Elem<BF16>::load(src, (r0 + r) * cols + c0 + lane) : 0.0f;
+        const float v = Elem<BF16>::load(src, in ? (r0 + r) * cols + c0 + lane : 0);
+        tile[r][lane] = in ? v : 0.0f;
     }
     __syncthreads();
     const int64_t c = c0 + (tid >> 2), kb = r0 / kMxBlock + (tid & 3);
