@@ -17,7 +17,7 @@ constexpr int kBackwardWaves = 4;
 constexpr int kMaxBackwardBlocks = 2048;
 // Waves of a block of the forward kernel: as many as its sums of p per wave leave room for in LDS and its registers on a compute unit, since a
 // block leaves one row of partial sums (sixteen waves a block on 256 blocks instead of four on 512, 512 experts: 92 -> 45 us).
-constexpr int route_waves(int V) { return V == 8 ? 16 : V == 16 ? 8 : 4; }
+constexpr int route_waves(int V, bool pieces) { return V == 8 ? 16 : V == 16 ? (pieces ? 16 : 8) : 4; }
 
 struct RouteArgs {
     const void* logits;
@@ -111,36 +111,44 @@ template <bool BF16, int V, bool VEC> struct RawRow {
     // its logits: -infinity for NaN, behind the row's end and in a row that takes no part; whether there are others
     __device__ __forceinline__ bool values(const RouteArgs& a, bool there, int gi, float (&l)[V], float* largest) const {
         const float ninf = -__builtin_inff();
+        const bool row_on = there && on;
         if constexpr (VEC) {
 #pragma unroll
-            for (int v = 0; v < V; v += VE) widen<BF16>(q[v / VE], l + v);
+            for (int v = 0; v < V; v += VE) {
+                widen<BF16>(q[v / VE], l + v);
+                const bool in = row_on && element<BF16, VEC>(v, gi, a.lanes) < a.E;
+#pragma unroll
+                for (int i = 0; i < VE; ++i) l[v + i] = in && l[v + i] == l[v + i] ? l[v + i] : ninf;
+            }
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) l[v] = Elem<BF16>::load(x, v);
+            for (int v = 0; v < V; ++v) {
+                l[v] = Elem<BF16>::load(x, v);
+                l[v] = row_on && element<BF16, VEC>(v, gi, a.lanes) < a.E && l[v] == l[v] ? l[v] : ninf;
+            }
         }
         float m = ninf;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const bool in = there && on && element<BF16, VEC>(v, gi, a.lanes) < a.E;
-            l[v] = in && l[v] == l[v] ? l[v] : ninf;
-            m = fmaxf(m, l[v]);
-        }
+        for (int v = 0; v < V; ++v) m = fmaxf(m, l[v]);
         m = group_max(m, a.lanes);
         *largest = m;
         return m > ninf;
     }
 };
 
-// exp(l - m) for l <= m, m > -infinity; logits of +infinity share the row.  The product with log2(e) is carried in two parts: rounded to
-// one, it would leave a relative error of up to 2^-19 where l lies far below m.
-__device__ __forceinline__ float relative(float l, float m) {
-    constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.925963033e-8f;
-    const float x = fmaxf(l - m, -200.0f);       // (exp(-200) is 0 in fp32)
-    const float y = x * kLog2e;
-    const float rest = fmaf(x, kLog2eRest, fmaf(x, kLog2e, -y));
-    const float r = __builtin_amdgcn_exp2f(y);
-    const float v = fmaf(r, rest * 0.693147181f, r);
-    return m == __builtin_inff() ? (l == m ? 1.0f : 0.0f) : v;
+// exp(l - m) for l <= m, m finite.  (The product with log2(e) is rounded once more: a relative 2^-24 |l - m|, as much as the difference's.)
+__device__ __forceinline__ float relative(float l, float m) { return __builtin_amdgcn_exp2f((l - m) * 1.44269504f); }
+// The same for any m: logits of +infinity share the row.
+__device__ __forceinline__ float share_of(float l, float m) { return m == __builtin_inff() ? (l == m ? 1.0f : 0.0f) : relative(l, m); }
+// All of a row's (zeros where it has none).
+template <int V> __device__ __forceinline__ void shares_of(const float (&l)[V], float m, bool any, float (&p)[V]) {
+    const float by = any ? m : 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = relative(l[v], by);
+    if (__any(m == __builtin_inff())) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) p[v] = share_of(l[v], by);
+    }
 }
 
 // order of LDS accesses within a wave (they execute in order; the compiler must keep them so)
@@ -160,8 +168,8 @@ template <bool BF16, int V, bool VEC> struct Picker {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const uint32_t b = __float_as_uint(row[v] + 0.0f);            // (-0 as 0)
-                const uint32_t up = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-                key[v] = row[v] > -__builtin_inff() ? (up & 0xffff0000u) | (0xffffu - (uint32_t)element<BF16, VEC>(v, gi, G)) : 0u;
+                const uint32_t up = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+                key[v] = (up & 0xffff0000u) | (0xffffu - (uint32_t)element<BF16, VEC>(v, gi, G));
             }
         } else {
             mine = -__builtin_inff();
@@ -181,7 +189,7 @@ template <bool BF16, int V, bool VEC> struct Picker {
             best = group_max(best, G);
 #pragma unroll
             for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0u : key[v];
-            *found = best != 0;
+            *found = best >= 0x00800000u;          // (above -infinity's 0x007f....)
             *at = 0xffff - (int)(best & 0xffffu);
             const uint32_t up = best & 0xffff0000u;
             *value = __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up & 0xffff0000u);
@@ -218,8 +226,8 @@ template <bool BF16, int V, bool VEC> struct Picker {
 };
 
 template <bool BF16, int V, bool VEC>
-__global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteArgs a) {
-    constexpr int kWaves = route_waves(V);
+__global__ __launch_bounds__(64 * route_waves(V, VEC)) void route_kernel(const RouteArgs a) {
+    constexpr int kWaves = route_waves(V, VEC);
     extern __shared__ float lds[];               // the slots chosen; statistics: kWaves x E sums, E counts
     __shared__ float block_z[kWaves];
     __shared__ int32_t block_n[kWaves];
@@ -253,11 +261,9 @@ __global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteA
         float total = 0;
         if (stats || !a.normalise) {
             float p[V];
+            shares_of(l, m, any, p);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                p[v] = any ? relative(l[v], m) : 0.0f;
-                total += p[v];
-            }
+            for (int v = 0; v < V; ++v) total += p[v];
             total = group_add(total, G);
             if (stats) {
                 const float inv = any ? 1.0f / total : 0.0f;
@@ -271,26 +277,30 @@ __global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteA
             }
         }
         Picker<BF16, V, VEC> picker(l, gi, G);
-        float chosen = 0;
         for (int i = 0; i < k; ++i) {
             float value;
             int at = 0;
             bool found;
             const bool mine = picker.next(gi, G, &value, &at, &found);
-            const float w = found ? relative(value, m) : 0.0f;
-            chosen += w;
             if (mine || (!found && gi == 0)) {
-                my_w[i] = w;
+                my_w[i] = value;
                 my_i[i] = found ? at : -1;
                 if (stats && found) atomicAdd(counts + at, 1);
             }
         }
         wave_sync();
+        // a lane a slot (k <= G), or several
+        float chosen = 0;
+        if (a.normalise) {
+            for (int i = gi; i < k; i += G) chosen += my_i[i] >= 0 ? share_of(my_w[i], m) : 0.0f;
+            chosen = group_add(chosen, G);
+        }
         const float by = a.normalise ? chosen : total;
         if (there)
             for (int i = gi; i < k; i += G) {
-                a.idx[t * k + i] = my_i[i];
-                a.weight[t * k + i] = any ? my_w[i] / by : 0.0f;
+                const int e = my_i[i];
+                a.idx[t * k + i] = e;
+                a.weight[t * k + i] = e >= 0 ? share_of(my_w[i], m) / by : 0.0f;
             }
         wave_sync();
     }
@@ -411,12 +421,31 @@ __global__ __launch_bounds__(256) void route_empty_kernel(int E, int32_t* __rest
     if (loss && e < 2) loss[e] = 0;
 }
 
-template <bool BF16, int V, bool VEC>
+// kSlots: slots of a row that a lane looks after (gi, gi + G, ...): one where k <= G, else up to eight (k <= E <= G V, and V = 8 where G < 32)
+template <bool BF16, int V, bool VEC, int kSlots>
 __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(const RouteArgs a) {
     extern __shared__ float patches[];           // G V words a group, zeros between rows
     constexpr int VE = BF16 ? 8 : 4, es = BF16 ? 2 : 4;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int G = a.lanes, gi = lane & (G - 1), rows = 64 / G, E = a.E, k = a.k;
+    // a row's logits, chosen experts and their gradients, asked for ahead of their use
+    int64_t t0 = ((int64_t)blockIdx.x * kBackwardWaves + wv) * rows;
+    RawRow<BF16, V, VEC> raw;
+    uint32_t next_e[kSlots];
+    float next_g[kSlots];
+    const auto ask = [&](int64_t t) {
+        raw.load(a, t, gi);
+        if (!a.dweight) return;
+        t = t < a.T ? t : a.T - 1;
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            if (s * G >= k) break;
+            const int i = gi + s * G;
+            next_e[s] = i < k ? (uint32_t)a.idx[t * k + i] : ~0u;
+            next_g[s] = i < k ? a.dweight[t * k + i] : 0.0f;
+        }
+    };
+    if (t0 < a.T) ask(t0 + lane / G);
     float* const patch = patches + (tid / G) * (G * V);
     for (int i = lane; i < 64 * V; i += 64) patches[wv * 64 * V + i] = 0;
     wave_sync();
@@ -436,38 +465,30 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
         }
     }
     const int64_t step = (int64_t)gridDim.x * kBackwardWaves * rows;
-    // slots of a row that this lane looks after: gi, gi + G, ... (k <= E <= G V, and k <= 32)
-    constexpr int kSlots = V == 8 ? 8 : 1;
-    for (int64_t t0 = ((int64_t)blockIdx.x * kBackwardWaves + wv) * rows; t0 < a.T; t0 += step) {
+    for (; t0 < a.T; t0 += step) {
         const int64_t t = t0 + lane / G;
         const bool there = t < a.T;
         const int64_t tt = there ? t : a.T - 1;
         const char* const row = (const char*)a.logits + tt * E * es;
-        RawRow<BF16, V, VEC> raw;
-        raw.load(a, t, gi);
-        // everything else that the row needs from memory is asked for before the first wait
         uint32_t slot_e[kSlots];
         float slot_g[kSlots], slot_x[kSlots];
         if (a.dweight) {
 #pragma unroll
             for (int s = 0; s < kSlots; ++s) {
                 if (s * G >= k) break;
-                const int i = gi + s * G;
-                slot_e[s] = i < k ? (uint32_t)a.idx[tt * k + i] : ~0u;
-                slot_g[s] = i < k ? a.dweight[tt * k + i] : 0.0f;
-            }
-#pragma unroll
-            for (int s = 0; s < kSlots; ++s) {
-                if (s * G >= k) break;
+                slot_e[s] = next_e[s];
+                slot_g[s] = next_g[s];
                 slot_x[s] = Elem<BF16>::load(row, slot_e[s] < (uint32_t)E ? slot_e[s] : 0);
             }
         }
         float l[V], d[V], m;
         const bool any = raw.values(a, there, gi, l, &m);
+        if (t0 + step < a.T) ask(t + step);
         float s = 0, dot = 0;
+        shares_of(l, m, any, d);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            l[v] = any ? relative(l[v], m) : 0.0f;
+            l[v] = d[v];
             s += l[v];
             dot = fmaf(l[v], pull[v], dot);
         }
@@ -485,7 +506,7 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
             for (int s = 0; s < kSlots; ++s) {
                 if (s * G >= k) break;
                 const bool good = any && slot_e[s] < (uint32_t)E && slot_x[s] == slot_x[s];
-                slot_x[s] = good ? relative(slot_x[s], m) : 0.0f;
+                slot_x[s] = good ? share_of(slot_x[s], m) : 0.0f;
                 slot_g[s] = any && slot_e[s] < (uint32_t)E ? slot_g[s] : 0.0f;         // (no expert's: not read)
                 sum += slot_x[s];
                 mean = fmaf(slot_x[s], slot_g[s], mean);
@@ -532,18 +553,19 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
     }
 }
 
-// Registers a lane (a power of two, 8 at least) and lanes a row.
+// Registers a lane (a power of two, 8 at least) and lanes a row.  A row on fewer lanes shares the steps over the lanes among more rows of a wave
+// (512 fp32 logits, 8 chosen: half a wave, 16 registers a lane).
 void route_shape(int64_t E, int* V, int* G) {
-    *V = E <= 512 ? 8 : E <= 1024 ? 16 : E <= 2048 ? 32 : 64;
+    *V = E <= 256 ? 8 : E <= 1024 ? 16 : E <= 2048 ? 32 : 64;
     int g = 1;
     while (g * *V < E) g *= 2;
     *G = g;
 }
 
-// Rows of partial sums that scratch has room for, and blocks of the forward kernel at most: one a compute unit.
+// Rows of partial sums that scratch has room for, and blocks of the forward kernel: one a compute unit (50432 tokens, 128 experts: 14.7 us; two: 17.4).
 constexpr int64_t kMaxPartRows = 256;
-int route_blocks(int64_t T, int V, int G) {
-    const int64_t rows = route_waves(V) * (64 / G), most = device_info().cus < kMaxPartRows ? device_info().cus : kMaxPartRows;
+int route_blocks(int64_t T, int waves, int G) {
+    const int64_t rows = waves * (64 / G), most = device_info().cus < kMaxPartRows ? device_info().cus : kMaxPartRows;
     const int64_t b = (T + rows - 1) / rows;
     return (int)(b > most ? most : b);
 }
@@ -622,7 +644,7 @@ hipError_t launch_route(const Route& r, int32_t* idx, float* weight, int32_t* co
         a.part_n = (int32_t*)(base + at.part_n);
         a.ticket = (int32_t*)(base + at.ticket);
     }
-    const int blocks = route_blocks(r.T, V, a.lanes), waves = route_waves(V);
+    const int waves = route_waves(V, vec), blocks = route_blocks(r.T, waves, a.lanes);
     const size_t lds = (size_t)waves * (64 / a.lanes) * r.k * 8 + (stats ? (size_t)(waves + 1) * r.E * 4 : 0);
     note_launch("route_kernel<%s,%d,%s>", r.bf16 ? "bf16" : "f32", V, vec ? "pieces" : "elements");
     hipError_t e = with_shape(r.bf16, V, vec, [&](auto B, auto N, auto X) {
@@ -657,7 +679,9 @@ hipError_t launch_route_backward(const Route& r, const int32_t* idx, const int32
     if (blocks > kMaxBackwardBlocks) blocks = kMaxBackwardBlocks;
     note_launch("route_backward_kernel<%s,%d,%s>", r.bf16 ? "bf16" : "f32", V, vec ? "pieces" : "elements");
     return with_shape(r.bf16, V, vec, [&](auto B, auto N, auto X) {
-        const auto kernel = route_backward_kernel<decltype(B)::value, decltype(N)::value, decltype(X)::value>;
+        constexpr bool bf16 = decltype(B)::value, pieces = decltype(X)::value;
+        constexpr int regs = decltype(N)::value;
+        const auto kernel = regs == 8 && r.k > a.lanes ? route_backward_kernel<bf16, regs, pieces, regs == 8 ? 8 : 1> : route_backward_kernel<bf16, regs, pieces, 1>;
         const size_t lds = (size_t)kBackwardWaves * 64 * decltype(N)::value * 4;
         if (lds > 60 * 1024) {
             const hipError_t rc = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

@@ -66,9 +66,10 @@ __device__ __forceinline__ bf16x8_t dequantise8(uint32_t codes, float scale) {
     return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+template <int BYTE = 0>
 __device__ __forceinline__ f32x4_t mfma4(const uint4& w, uint32_t ws, const uint4& a, uint32_t as, const f32x4_t& acc) {
     const i32x8_t vw = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0}, va = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, va, acc, 4, 4, 0, (int)ws, 0, (int)as);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, va, acc, 4, 4, BYTE, (int)ws, BYTE, (int)as);
 }
 
 // One step of 128 elements: a block of 32 of this lane's row of W against MT rows of A (A in bf16: four pieces each).
@@ -302,37 +303,36 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
 // ---- tiles through LDS -------------------------------------------------------------------------------------
 //
 // Many rows of A: a block of four waves takes 16 MT rows of A against 128 rows of W, a wave all of these rows of A against 32 of W (so that codes
-// are converted once a block).  A stage is 64 elements of K (bf16 rows: 128 bytes of a row of A, 32 of W) or 128 (codes: 64 bytes of either); of the
-// three stages in LDS one is multiplied and two are on their way, straight from memory.  Two blocks share a compute unit, and one multiplies while the
-// other waits or ends.  (4096 x 4096 x 4096 and 16384 x 2048 x 768 of bf16 rows, 8192 x 4096 x 4096 of codes: 134, 59 and 117 us; a wave on 64 x 64: 145,
-// 61, 131; eight waves on 256 x 256, half of them reading while the others multiply: 138, 65, 134; all three before the panels below.)
+// are converted once a block).  A stage is 64 elements of K of bf16 rows (128 bytes of a row of A, 32 of W), 256 of codes (128 bytes of either): one is
+// multiplied while the others in LDS, two or one, are on their way straight from memory.  Two blocks share a compute unit, and one multiplies while the
+// other waits or ends.  4096 x 4096 x 4096 and 16384 x 2048 x 768 of bf16 rows, 8192 x 4096 x 4096 of codes, us on one card before the next two
+// points: 134, 59 and 117; a wave on 64 x 64 results: 145, 61, 131; eight waves on 256 x 256, half of them reading while the others multiply: 138, 65, 134.
+// Stages of 128 elements of codes, three of them: 152 us instead of 116 (twice the barriers).
 // Scale bytes come in panels of 32 blocks (1024 elements of K) of every row, with the first stage that they belong to: a row's scales of one stage are
 // a few bytes in a line of their own, so that fetching them stage by stage cost as much as the codes (8192 x 4096 x 4096, four bits both: 121 us without
 // such loads, 174 with them), and a panel of the whole K before the first stage was a third of a short K's time (16384 x 768 x 2048: 87 -> 71 us).
 //
 // Lane (j, g) multiplies, of a stage of bf16 rows, elements 16 g + 8 u .. + 7 in step u (pieces 2 g + u of A, four bytes of codes); of a stage of codes,
-// block g.  Pieces of 16 bytes in LDS are turned within their row so that the 16 lanes of a pass of an operand read (rows
-// {0-3, 12-15} of one g with rows {4-11} of its neighbour, then the others) meet every bank once; the turn is made by
-// the lanes' source addresses, since a load to LDS writes lane after lane: 128-byte rows as tile_swz, 64-byte rows by 2 (row >> 3 & 1), 32-byte rows
-// (read eight bytes a lane) not at all.
+// block 2 g + u.  Pieces of 16 bytes in LDS are turned within their row as tile_swz has it, so that the 16 lanes of a pass of an operand read meet every
+// bank once; the turn is made by the lanes' source addresses, since a load to LDS writes lane after lane.  Rows of 32 bytes, read eight bytes a lane, need none.
 __device__ const uint4 g_zero_piece = {0, 0, 0, 0};
 constexpr int kPanel = 32;       // blocks whose scales come together
 
-template <int ROW> __device__ __forceinline__ int turn(int row) { return ROW == 128 ? lds_rot(row) : ROW == 64 ? 2 * ((row >> 3) & 1) : 0; }
+template <int ROW> __device__ __forceinline__ int turn(int row) { return ROW == 128 ? lds_rot(row) : 0; }
 template <int ROW> __device__ __forceinline__ int lds_slot(int row, int piece) {
     constexpr int n = ROW / 16;
     return row * n + ((piece + turn<ROW>(row)) & (n - 1));
 }
 template <bool A4, int MT> struct TileShape {
     static constexpr int kThreads = 256, kWaves = 4, NT = 2, kRows = 16 * MT, kCols = 128;
-    static constexpr int kARow = A4 ? 64 : 128, kWRow = A4 ? 64 : 32;           // bytes of a row in a stage
-    static constexpr int kStageBlocks = A4 ? 4 : 2;                               // blocks of 32 in a stage
+    static constexpr int kARow = 128, kWRow = A4 ? 128 : 32, kRing = A4 ? 2 : 3;           // bytes of a row in a stage
+    static constexpr int kStageBlocks = A4 ? 8 : 2;                               // blocks of 32 in a stage
     static constexpr int kABytes = kRows * kARow, kWBytes = kCols * kWRow, kStage = kABytes + kWBytes;
     static constexpr int kALoads = kABytes / 1024 / kWaves, kWLoads = kWBytes / 1024 / kWaves;   // a wave's loads of 1 KB a stage
     static_assert(kALoads * 1024 * kWaves == kABytes && kWLoads * 1024 * kWaves == kWBytes, "whole loads a wave");
     static constexpr int kScaleRows = kCols + (A4 ? 128 : 0);      // (rows behind the last: its scales again)
     static constexpr int kPanelBytes = kScaleRows * kPanel, kPanelStages = kPanel / kStageBlocks, kPanelLoads = kPanelBytes / 1024 / kWaves, kPanelWords = kPanelBytes / 256 / kWaves;
-    static constexpr int kLds = 3 * kStage + 2 * kPanelBytes;
+    static constexpr int kLds = kRing * kStage + 2 * kPanelBytes;
 };
 
 template <bool A4, int MODE, bool WIDE, int MT>
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
 #pragma unroll
     for (int i = 0; i < S::kPanelLoads; ++i) s_src[i] = (const char*)scales_of((i * S::kWaves + wv) * 32 + lane / 2) + 16 * (lane % 2);
     const auto fetch_panel = [&](int panel) {
-        const int b0 = panel * kPanel, to = 3 * S::kStage + (panel & 1) * S::kPanelBytes;
+        const int b0 = panel * kPanel, to = S::kRing * S::kStage + (panel & 1) * S::kPanelBytes;
         if (scale_width == 16) {
 #pragma unroll
             for (int i = 0; i < S::kPanelLoads; ++i)
@@ -463,32 +463,34 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int kLoads = S::kALoads + S::kWLoads, kSteps = A4 ? 1 : 2;
-    uint4 fa[kSteps][MT], fw[NT];        // (bf16 rows: fw[.].xy are the codes of both steps of a stage)
-    uint32_t as[MT], ws[NT];
+    constexpr int kLoads = S::kALoads + S::kWLoads, kSteps = 2;
+    uint4 fa[kSteps][MT], fw[A4 ? 2 : 1][NT];        // (bf16 rows: fw[.].xy are the codes of both steps of a stage)
+    uint32_t as[MT], ws[NT];      // (A4: the bytes of both steps)
     const auto read = [&](int c, int buf) {
         const uint4* const la = (const uint4*)(lds + buf * S::kStage);
         const char* const lw = lds + buf * S::kStage + S::kABytes;
-        const uint8_t* const scales = (const uint8_t*)lds + 3 * S::kStage + (c / S::kPanelStages & 1) * S::kPanelBytes + c * S::kStageBlocks % kPanel;
-        const int b = A4 ? g : g >> 1;
+        const uint8_t* const scales = (const uint8_t*)lds + S::kRing * S::kStage + (c / S::kPanelStages & 1) * S::kPanelBytes + c * S::kStageBlocks % kPanel;
+        const int b = A4 ? 2 * g : g >> 1;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int row = 16 * (wv * NT + n) + j;
             if constexpr (A4) {
-                fw[n] = ((const uint4*)lw)[lds_slot<64>(row, g)];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) fw[u][n] = ((const uint4*)lw)[lds_slot<128>(row, 2 * g + u)];
+                ws[n] = *(const uint16_t*)(scales + row * kPanel + b);
             } else {
                 const uint2 v = *(const uint2*)(lw + row * 32 + 8 * g);
-                fw[n].x = v.x;
-                fw[n].y = v.y;
+                fw[0][n].x = v.x;
+                fw[0][n].y = v.y;
+                ws[n] = scales[row * kPanel + b];
             }
-            ws[n] = scales[row * kPanel + b];
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int row = 16 * m + j;
 #pragma unroll
-            for (int u = 0; u < kSteps; ++u) fa[u][m] = la[A4 ? lds_slot<64>(row, g) : lds_slot<128>(row, 2 * g + u)];
-            if constexpr (A4) as[m] = scales[(S::kCols + row) * kPanel + b];
+            for (int u = 0; u < kSteps; ++u) fa[u][m] = la[lds_slot<128>(row, 2 * g + u)];
+            if constexpr (A4) as[m] = *(const uint16_t*)(scales + (S::kCols + row) * kPanel + b);
         }
     };
     const auto multiply = [&]() {
@@ -498,9 +500,9 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
             for (int n = 0; n < NT; ++n) {
                 if constexpr (A4) {
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[n][m] = mfma4(fw[n], ws[n], fa[0][m], as[m], acc[n][m]);
+                    for (int m = 0; m < MT; ++m) acc[n][m] = u == 0 ? mfma4<0>(fw[u][n], ws[n], fa[u][m], as[m], acc[n][m]) : mfma4<1>(fw[u][n], ws[n], fa[u][m], as[m], acc[n][m]);
                 } else {
-                    const bf16x8_t f = dequantise8(u == 0 ? fw[n].x : fw[n].y, __uint_as_float(ws[n] << 23));
+                    const bf16x8_t f = dequantise8(u == 0 ? fw[0][n].x : fw[0][n].y, __uint_as_float(ws[n] << 23));
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
                         acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, __builtin_bit_cast(bf16x8_t, fa[u][m]), acc[n][m], 0, 0, 0);
@@ -520,8 +522,8 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
     for (int q = 0; q < 8; ++q)
         bias[q] = n8 + q >= a.N ? 0.f : MODE == kDense ? bias_at(a, a.bias, n8 + q) : bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n8 + q]);
 #pragma unroll 1
-    for (int c = 0; c < 3 && c < stages; ++c) fetch(c, c);
-    if (stages > 2) wait_loads<2 * kLoads>();
+    for (int c = 0; c < S::kRing && c < stages; ++c) fetch(c, c);
+    if (stages >= S::kRing) wait_loads<(S::kRing - 1) * kLoads>();
     else wait_loads<0>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     barrier();
@@ -530,14 +532,14 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
         read(c, buf);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         // this wave's part of stage c + 1 is there (stage c + 2 may be on its way, with a panel of scales or without)
-        if (c + 2 >= stages) wait_loads<0>();
+        if (S::kRing == 2 || c + 2 >= stages) wait_loads<0>();
         else if ((c + 2) % S::kPanelStages != 0 || scale_width == 1) wait_loads<kLoads>();
         else if (scale_width == 16) wait_loads<kLoads + S::kPanelLoads>();
         else wait_loads<kLoads + S::kPanelWords>();
         barrier();
-        if (c + 3 < stages) fetch(c + 3, buf);      // (everybody has read stage c)
+        if (c + S::kRing < stages) fetch(c + S::kRing, buf);      // (everybody has read stage c)
         multiply();
-        buf = buf == 2 ? 0 : buf + 1;
+        buf = buf == S::kRing - 1 ? 0 : buf + 1;
     }
 
     // Results through LDS, half of the wave's rows at a time, so that they leave as whole rows of 16 NT columns, eight a lane, from a loop:
@@ -984,7 +986,21 @@ template <bool A4, int MODE> hipError_t launch_rows(const Args& a, int64_t tiles
     return hipGetLastError();
 }
 
-int rows_tile(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+// Times in us of a product by mx4_rows_kernel and by mx4_tile_kernel, fitted to both over 16 .. 256 rows, 4096 x 4096 and 1024 x 768 matrices (bf16 rows and
+// codes; within about 10 %): the one grows with its rows from a launch's time on, the other is a chain of stages along K until its tiles fill the
+// chip more than once.  (4096 x 4096, bf16 rows: 96 of them 31 / 34 us, 128 37 / 34; codes: 64 11.8 / 13.6, 96 18.0 / 13.6; 1024 x 768, bf16 rows: 256 6.7 / 12.1.)
+double rows_us(bool a4, double rows, int64_t N, int64_t K) { return 4.2 + rows * (double)N * (double)K * (a4 ? 7.9e-9 : 1.55e-8); }
+double tiles_us(bool a4, double rows64, int64_t N, int64_t K) {
+    const double tiles = rows64 * (double)((N + 127) / 128) / 512;
+    return 5 + (double)K * (a4 ? 0.0021 : 0.007) * (tiles > 1 ? tiles : 1);
+}
+
+// Rows of A a block of mx4_rows_kernel takes, in tiles of 16: the most that leave blocks for three quarters of the compute units (1024 x 768, bf16 rows, one, two
+// and four tiles: 64 rows 4.4, 4.9, 6.6 us; 128 5.9, 5.0, 6.6; 256 8.2, 7.2, 6.7).
+int rows_tile(int64_t rows, int64_t N) {
+    const auto fills = [&](int mt) { return (rows + 16 * mt - 1) / (16 * mt) * ((N + 15) / 16) >= kSmallEnoughBlocks; };
+    return rows > 32 && fills(4) ? 4 : rows > 16 && fills(2) ? 2 : 1;
+}
 
 int64_t align256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -1031,12 +1047,12 @@ hipError_t launch_mx4_product(const Mx4Product& p, hipStream_t s) {
     a.act = p.act;
     a.out_bf16 = p.out_bf16;
     a.out_vec = p.N % 4 == 0 && ((uintptr_t)p.out & (p.out_bf16 ? 7 : 15)) == 0;
-    if (p.T >= 128) {
+    if (tiles_us(a4, (double)((p.T + 63) / 64), p.N, p.K) < rows_us(a4, (double)p.T, p.N, p.K)) {
         const int tile_rows = tile_rows_for(p.T, p.N);
         const int64_t tiles = (p.T + tile_rows - 1) / tile_rows;
         return a4 ? launch_tiles<true, kDense>(a, tiles, tile_rows, s) : launch_tiles<false, kDense>(a, tiles, tile_rows, s);
     }
-    const int mt = rows_tile(p.T);
+    const int mt = rows_tile(p.T, p.N);
     const int64_t tiles = (p.T + 16 * mt - 1) / (16 * mt);
     return a4 ? launch_rows<true, kDense>(a, tiles, mt, s) : launch_rows<false, kDense>(a, tiles, mt, s);
 }
@@ -1092,10 +1108,12 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
         if ((e = launch_direct<true>(a, P, s)) != hipSuccess) return e;
         return launch_direct<false>(b, p.T, s);
     }
-    const bool large = P / p.E >= 64;
-    const int mt = rows_tile(P / p.E);
+    const int64_t met = p.E < P ? p.E : P;
+    const int mt = P / p.E <= 16 ? 1 : P / p.E <= 32 ? 2 : 4;
+    const double rows = 16.0 * mt * (double)(P / (16 * mt) + met), rows64 = (double)(P / 64 + met);
+    const bool large = tiles_us(false, rows64, p.L, p.D) + tiles_us(false, rows64, p.O, p.L) < rows_us(false, rows, p.L, p.D) + rows_us(false, rows, p.O, p.L);
     const int tile_rows = large ? tile_rows_for(P, p.L < p.O ? p.L : p.O) : 16 * mt;
-    const int64_t tiles = P / tile_rows + (p.E < P ? p.E : P);
+    const int64_t tiles = P / tile_rows + met;
     int32_t *const count = words(at.count), *const start = words(at.start), *const tile_start = words(at.tile_start);
     int32_t *const rank = words(at.rank), *const perm = words(at.perm), *const tile_leaf = words(at.tile_leaf), *const tile_slot = words(at.tile_slot);
     if (P <= kGroupOnePairs && p.E <= kGroupOneLeaves) {

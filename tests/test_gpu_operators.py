@@ -122,7 +122,8 @@ def _matrix(rng, shape, scale):
     return c, s, R.values(c, s, shape[-1])
 
 
-SIZES = [(1, 32, 16), (1, 8192, 64), (130, 4160, 140), (150, 8230, 40), (3000, 264, 3200), (2050, 100, 4100), (1, 4096, 256), (3, 31, 5), (16, 128, 64), (17, 100, 33), (31, 160, 48), (33, 1000, 77), (64, 96, 130), (65, 257, 31),
+SIZES = [(1, 32, 16), (1, 8192, 64), (130, 4160, 140), (150, 8230, 40), (3000, 264, 3200), (2050, 100, 4100),
+         (700, 1024, 1100), (900, 1030, 1000), (150, 4096, 4100), (1200, 40, 900), (1, 4096, 256), (3, 31, 5), (16, 128, 64), (17, 100, 33), (31, 160, 48), (33, 1000, 77), (64, 96, 130), (65, 257, 31),
          (129, 512, 257), (200, 777, 129), (257, 2048, 96), (300, 64, 515), (513, 320, 256)]
 
 
@@ -225,6 +226,7 @@ LEAVES = [
     (150, 1, 3,  160, 130, 257, True),
     (700, 2, 5,  296, 136, 300, True),
     (4100, 8, 2, 136, 1032, 1100, True),
+    (900, 2, 3, 1024, 640, 900, True),
     # more pairs, or leaves, than one block groups
     (4200, 8, 8, 40,  24,  16,  True),
     (5001, 8, 4100, 32, 16, 8,  True),
