@@ -304,10 +304,11 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
 //
 // Many rows of A: a block of four waves takes 16 MT rows of A against 128 rows of W, a wave all of these rows of A against 32 of W (so that codes
 // are converted once a block).  A stage is 64 elements of K of bf16 rows (128 bytes of a row of A, 32 of W), 256 of codes (128 bytes of either): one is
-// multiplied while the others in LDS, two or one, are on their way straight from memory.  Two blocks share a compute unit, and one multiplies while the
-// other waits or ends.  4096 x 4096 x 4096 and 16384 x 2048 x 768 of bf16 rows, 8192 x 4096 x 4096 of codes, us on one card before the next two
-// points: 134, 59 and 117; a wave on 64 x 64 results: 145, 61, 131; eight waves on 256 x 256, half of them reading while the others multiply: 138, 65, 134.
-// Stages of 128 elements of codes, three of them: 152 us instead of 116 (twice the barriers).
+// multiplied while the next is on its way straight from memory to LDS.  Three blocks (of codes two) share a compute unit, and one multiplies while another
+// waits or ends.  What that is worth, in us, for 16384 x 768 x 2048 with GELU, 16384 x 2048 x 768 and 4096 x 4096 x 4096 of bf16 rows: 78, 53, 139; two blocks
+// with three stages 92, 61, 141; before both, on another card, a wave on 64 x 64 results and eight waves on 256 x 256 of them, half of which read
+// while the others multiply, took 116, 61, 145 and 97, 65, 138 where this shape took 106, 59, 134.
+// 8192 x 4096 x 4096 of codes: 109; three stages of 128 elements (twice the barriers) 152 where this took 116.
 // Scale bytes come in panels of 32 blocks (1024 elements of K) of every row, with the first stage that they belong to: a row's scales of one stage are
 // a few bytes in a line of their own, so that fetching them stage by stage cost as much as the codes (8192 x 4096 x 4096, four bits both: 121 us without
 // such loads, 174 with them), and a panel of the whole K before the first stage was a third of a short K's time (16384 x 768 x 2048: 87 -> 71 us).
@@ -325,7 +326,8 @@ template <int ROW> __device__ __forceinline__ int lds_slot(int row, int piece) {
 }
 template <bool A4, int MT> struct TileShape {
     static constexpr int kThreads = 256, kWaves = 4, NT = 2, kRows = 16 * MT, kCols = 128;
-    static constexpr int kARow = 128, kWRow = A4 ? 128 : 32, kRing = A4 ? 2 : 3;           // bytes of a row in a stage
+    static constexpr int kARow = 128, kWRow = A4 ? 128 : 32;           // bytes of a row in a stage
+    static constexpr int kRing = 2;                                                // stages in LDS
     static constexpr int kStageBlocks = A4 ? 8 : 2;                               // blocks of 32 in a stage
     static constexpr int kABytes = kRows * kARow, kWBytes = kCols * kWRow, kStage = kABytes + kWBytes;
     static constexpr int kALoads = kABytes / 1024 / kWaves, kWLoads = kWBytes / 1024 / kWaves;   // a wave's loads of 1 KB a stage
@@ -336,7 +338,7 @@ template <bool A4, int MT> struct TileShape {
 };
 
 template <bool A4, int MODE, bool WIDE, int MT>
-__global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const uint32_t row_tiles, const uint32_t col_tiles) {
+__global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a, const uint32_t row_tiles, const uint32_t col_tiles) {
     typedef TileShape<A4, MT> S;
     constexpr int NT = S::NT;
     extern __shared__ __align__(16) char lds[];
@@ -403,15 +405,12 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
     const uintptr_t scale_bits = (uintptr_t)a.w_scales | (A4 ? (uintptr_t)a.a_scales : 0) | (uintptr_t)a.Kb;
     const int scale_width = scale_bits % 16 == 0 ? 16 : scale_bits % 4 == 0 ? 4 : 1;
     const auto scales_of = [&](int row) { return row < S::kCols ? a.w_scales + w_index(row) * a.Kb : a.a_scales + a_index(row - S::kCols) * a.Kb; };
-    const char* s_src[S::kPanelLoads];
-#pragma unroll
-    for (int i = 0; i < S::kPanelLoads; ++i) s_src[i] = (const char*)scales_of((i * S::kWaves + wv) * 32 + lane / 2) + 16 * (lane % 2);
     const auto fetch_panel = [&](int panel) {
         const int b0 = panel * kPanel, to = S::kRing * S::kStage + (panel & 1) * S::kPanelBytes;
         if (scale_width == 16) {
 #pragma unroll
             for (int i = 0; i < S::kPanelLoads; ++i)
-                load_to_lds(b0 + 16 * (lane % 2) < a.Kb ? s_src[i] + b0 : (const char*)&g_zero_piece,
+                load_to_lds(b0 + 16 * (lane % 2) < a.Kb ? (const char*)scales_of((i * S::kWaves + wv) * 32 + lane / 2) + 16 * (lane % 2) + b0 : (const char*)&g_zero_piece,
                             __builtin_amdgcn_readfirstlane(lds_address(lds) + to + (i * S::kWaves + wv) * 1024));
             return;
         }
@@ -514,13 +513,6 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
         asm volatile("s_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    // (the epilogue's: asked for here, where the wait for them is the stages')
-    constexpr int kLanes = 2 * NT;
-    const int64_t n8 = n0 + 16 * NT * wv + 8 * (lane % kLanes);
-    float bias[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-        bias[q] = n8 + q >= a.N ? 0.f : MODE == kDense ? bias_at(a, a.bias, n8 + q) : bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n8 + q]);
 #pragma unroll 1
     for (int c = 0; c < S::kRing && c < stages; ++c) fetch(c, c);
     if (stages >= S::kRing) wait_loads<(S::kRing - 1) * kLoads>();
@@ -531,11 +523,7 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
     for (int c = 0; c < stages; ++c) {
         read(c, buf);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        // this wave's part of stage c + 1 is there (stage c + 2 may be on its way, with a panel of scales or without)
-        if (S::kRing == 2 || c + 2 >= stages) wait_loads<0>();
-        else if ((c + 2) % S::kPanelStages != 0 || scale_width == 1) wait_loads<kLoads>();
-        else if (scale_width == 16) wait_loads<kLoads + S::kPanelLoads>();
-        else wait_loads<kLoads + S::kPanelWords>();
+        wait_loads<0>();               // this wave's part of stage c + 1 is there
         barrier();
         if (c + S::kRing < stages) fetch(c + S::kRing, buf);      // (everybody has read stage c)
         multiply();
@@ -545,10 +533,16 @@ __global__ __launch_bounds__(256, 2) void mx4_tile_kernel(const Args a, const ui
     // Results through LDS, half of the wave's rows at a time, so that they leave as whole rows of 16 NT columns, eight a lane, from a loop:
     // written out for every accumulator the epilogue was more code than the instruction cache takes, and fetching it took longer than
     // the stages of a short K.
+    constexpr int kLanes = 2 * NT;
     constexpr int kHalf = MT / 2, kPitch = 16 * NT + 4, kRowsAtOnce = 64 / kLanes;
     static_assert(S::kWaves * 16 * kHalf * kPitch * 4 <= S::kLds, "results fit where the stages were");
     float* const part = (float*)lds + wv * 16 * kHalf * kPitch;
     const int64_t limit = MODE == kHidden ? a.out_row : a.N;
+    const int64_t n8 = n0 + 16 * NT * wv + 8 * (lane % kLanes);
+    float bias[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        bias[q] = n8 + q >= a.N ? 0.f : MODE == kDense ? bias_at(a, a.bias, n8 + q) : bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n8 + q]);
     __syncthreads();
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -597,8 +591,8 @@ template <bool A4, int MODE, int MT> hipError_t launch_tiles(Args a, int64_t row
     return hipGetLastError();
 }
 
-// Rows of A a tile: 128 once there are enough such tiles for two a compute unit, else 64 (512 x 4096 x 4096 of bf16 rows, 128 or 256 tiles: 46 or
-// 33 us; 16384 x 2048 x 768, 768 or 1536 tiles: 59 or 63).
+// Rows of A a tile: 128 once there are enough such tiles for two a compute unit, else 64 (us with 64 / 128; K = N = 4096: 1024 bf16 rows, 256 tiles of 128,
+// 45 / 50, 2048 rows 76 / 67; of codes 20 / 23, 37 / 31; 4096 bf16 rows of 768, 2048 results, 512 tiles: 21 / 22).
 int tile_rows_for(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128) >= 2 * device_info().cus ? 128 : 64; }
 
 template <bool A4, int MODE> hipError_t launch_tiles(const Args& a, int64_t row_tiles, int tile_rows, hipStream_t s) {
@@ -668,7 +662,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
                 ws_row[u] = a.w_scales + r * a.Kb;
                 acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
-            tiles_steps(w_row, ws_row, h_tiles - t0 < kTokenTiles ? h_tiles - t0 : kTokenTiles, a.a + t * a.a_row, a.Kb, a.pieces, g, wv, kTokenWaves, acc);
+            tiles_steps<kTokenTiles>(w_row, ws_row, h_tiles - t0 < kTokenTiles ? h_tiles - t0 : kTokenTiles, a.a + t * a.a_row, a.Kb, a.pieces, g, wv, kTokenWaves, acc);
             if (j == 0) {
 #pragma unroll
                 for (int u = 0; u < kTokenTiles; ++u) *(f32x4_t*)&part[round][wv][16 * u + 4 * g] = acc[u];
@@ -707,7 +701,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
                 w_row[u] = b.w + r * b.Kb * 16;
                 ws_row[u] = b.w_scales + r * b.Kb;
             }
-            tiles_steps(w_row, ws_row, tiles, (const char*)(h + i * h_row), b.Kb, b.pieces, g, 0, 1, acc);
+            tiles_steps<kTokenTiles>(w_row, ws_row, tiles, (const char*)(h + i * h_row), b.Kb, b.pieces, g, 0, 1, acc);
             if (j == 0) {
 #pragma unroll
                 for (int u = 0; u < kTokenTiles; ++u)
@@ -800,7 +794,7 @@ template <bool HIDDEN> hipError_t launch_direct(const Args& a, int64_t items, hi
 //
 // rank[p] = place of pair p among its leaf's; which pair gets which place depends on the order of the atomics, and
 // nothing else does: a row's sums do not know its place in a tile.
-constexpr int kGroupPairs = 1024;         // pairs of a block of group_count_kernel
+constexpr int kGroupPairs = 1024;         // pairs of a block
 constexpr int kGroupLdsLeaves = 8192;     // leaves whose counts fit LDS
 
 // Counts of a block's pairs meet in LDS first (LDS: E <= kGroupLdsLeaves): 16384 pairs on 16 leaves, all by atomics on memory, took 46 us.
@@ -909,6 +903,50 @@ __global__ __launch_bounds__(256) void group_place_kernel(const int32_t* __restr
     if (e < E) place(p, e, rank[p], tile_rows, start, tile_start, perm, tile_leaf, tile_slot);
 }
 
+// Two launches while all blocks' counts are few: each block's own, then every block adds up those before it, scans the leaves and places its pairs.
+constexpr int64_t kGroupWords = 8192;     // counts of all blocks
+__global__ __launch_bounds__(1024) void group_hist_kernel(const int32_t* __restrict__ idx, int64_t P, int E, int32_t* __restrict__ counts) {
+    extern __shared__ int32_t own[];
+    for (int e = threadIdx.x; e < E; e += 1024) own[e] = 0;
+    __syncthreads();
+    const int64_t p = (int64_t)blockIdx.x * kGroupPairs + threadIdx.x;
+    const uint32_t e = p < P ? (uint32_t)idx[p] : ~0u;
+    if (e < (uint32_t)E) atomicAdd(own + e, 1);
+    __syncthreads();
+    for (int l = threadIdx.x; l < E; l += 1024) counts[(int64_t)blockIdx.x * E + l] = own[l];
+}
+
+__global__ __launch_bounds__(1024) void group_spread_kernel(const int32_t* __restrict__ idx, int64_t P, int E, int tile_rows,
+                                                            const int32_t* __restrict__ counts, int32_t* __restrict__ start,
+                                                            int32_t* __restrict__ tile_start, int32_t* __restrict__ perm,
+                                                            int32_t* __restrict__ tile_leaf, int32_t* __restrict__ tile_slot) {
+    extern __shared__ int32_t own[];          // places before this block's [E], all [E], start [E + 1], tile_start [E + 1]
+    __shared__ int32_t sums[2][16];
+    int32_t *const all = own + E, *const lds_start = all + E, *const lds_tiles = lds_start + E + 1;
+    for (int e = threadIdx.x; e < E; e += 1024) {
+        int32_t before = 0, total = 0;
+#pragma unroll 8
+        for (int b = 0; b < (int)gridDim.x; ++b) {
+            const int32_t n = counts[(int64_t)b * E + e];
+            before += b < (int)blockIdx.x ? n : 0;
+            total += n;
+        }
+        own[e] = before;
+        all[e] = total;
+    }
+    __syncthreads();
+    scan_leaves(all, E, tile_rows, lds_start, lds_tiles, sums);
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int e = threadIdx.x; e <= E; e += 1024) {
+            start[e] = lds_start[e];
+            tile_start[e] = lds_tiles[e];
+        }
+    const int64_t p = (int64_t)blockIdx.x * kGroupPairs + threadIdx.x;
+    const uint32_t e = p < P ? (uint32_t)idx[p] : ~0u;
+    if (e < (uint32_t)E) place(p, e, atomicAdd(own + e, 1), tile_rows, lds_start, lds_tiles, perm, tile_leaf, tile_slot);
+}
+
 // All of it in one block, for few pairs: counts, sums and places in LDS (a second pass of atomics gives the places).
 constexpr int64_t kGroupOnePairs = 4096, kGroupOneLeaves = 4096;
 __global__ __launch_bounds__(1024) void group_one_kernel(const int32_t* __restrict__ idx, int P, int E, int tile_rows, int32_t* __restrict__ start,
@@ -988,11 +1026,12 @@ template <bool A4, int MODE> hipError_t launch_rows(const Args& a, int64_t tiles
 
 // Times in us of a product by mx4_rows_kernel and by mx4_tile_kernel, fitted to both over 16 .. 256 rows, 4096 x 4096 and 1024 x 768 matrices (bf16 rows and
 // codes; within about 10 %): the one grows with its rows from a launch's time on, the other is a chain of stages along K until its tiles fill the
-// chip more than once.  (4096 x 4096, bf16 rows: 96 of them 31 / 34 us, 128 37 / 34; codes: 64 11.8 / 13.6, 96 18.0 / 13.6; 1024 x 768, bf16 rows: 256 6.7 / 12.1.)
+// chip more than once.  (4096 x 4096, bf16 rows: 96 of them 31 / 31 us, 128 36 / 31; codes: 64 11.7 / 13.8, 96 17.6 / 13.6; 768 x 2048, bf16 rows: 256
+// 9.0 / 10.4, 512 15.4 / 10.7; codes: 256 5.5 / 7.8, 1024 12.8 / 8.5.)
 double rows_us(bool a4, double rows, int64_t N, int64_t K) { return 4.2 + rows * (double)N * (double)K * (a4 ? 7.9e-9 : 1.55e-8); }
 double tiles_us(bool a4, double rows64, int64_t N, int64_t K) {
     const double tiles = rows64 * (double)((N + 127) / 128) / 512;
-    return 5 + (double)K * (a4 ? 0.0021 : 0.007) * (tiles > 1 ? tiles : 1);
+    return (a4 ? 6 : 7) + (double)K * (a4 ? 0.0019 : 0.0059) * (tiles > 1 ? tiles : 1);
 }
 
 // Rows of A a block of mx4_rows_kernel takes, in tiles of 16: the most that leave blocks for three quarters of the compute units (1024 x 768, bf16 rows, one, two
@@ -1014,7 +1053,7 @@ struct LeafScratch {
             return at;
         };
         const int64_t tiles = P / 16 + (E < P ? E : P) + 1;
-        count = take(4 * E);
+        count = take(4 * (E > kGroupWords ? E : kGroupWords));
         start = take(4 * (E + 1));
         tile_start = take(4 * (E + 1));
         rank = take(4 * P);
@@ -1119,6 +1158,13 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     if (P <= kGroupOnePairs && p.E <= kGroupOneLeaves) {
         note_launch("group_one_kernel");
         group_one_kernel<<<1, 1024, (size_t)(3 * p.E + 2) * 4, s>>>(p.idx, (int)P, (int)p.E, tile_rows, start, tile_start, perm, tile_leaf, tile_slot);
+    } else if ((P + kGroupPairs - 1) / kGroupPairs * p.E <= kGroupWords) {
+        const dim3 blocks((unsigned)((P + kGroupPairs - 1) / kGroupPairs));
+        note_launch("group_hist_kernel");
+        group_hist_kernel<<<blocks, 1024, (size_t)p.E * 4, s>>>(p.idx, P, (int)p.E, count);
+        note_launch("group_spread_kernel");
+        group_spread_kernel<<<blocks, 1024, (size_t)(4 * p.E + 2) * 4, s>>>(p.idx, P, (int)p.E, tile_rows, count, start, tile_start, perm, tile_leaf,
+                                                                             tile_slot);
     } else {
         if ((e = launch_zero(count, (p.E + 3) / 4 * 4, s)) != hipSuccess) return e;   // (whole pieces: the region is of 256 bytes)
         note_launch("group kernels");

@@ -230,6 +230,8 @@ LEAVES = [
     # more pairs, or leaves, than one block groups
     (4200, 8, 8, 40,  24,  16,  True),
     (5001, 8, 4100, 32, 16, 8,  True),
+    (5003, 8, 700, 32, 16, 8,   False),
+    (2100, 2, 40, 32, 16, 8,    True),
     (4700, 8, 9000, 32, 16, 8,  True),
 ]
 
