@@ -289,6 +289,31 @@ def test_leaves_a_vector_of_indices_and_no_token_with_a_leaf():
             assert not out.any()
 
 
+@pytest.mark.parametrize("E,T", [(4090, 60), (8000, 60), (4001, 1500), (3999, 2000), (20000, 90)])
+def test_leaves_few_tokens_of_many_wide_leaves(E, T):
+    """More leaves than the small groupings' tables hold.  Matrices of zeros: a token is the mixture of its leaves' last biases."""
+    import torch
+    import paper_2308_14711_amd as F
+    D, L, O, k = 2048, 260, 520, 2
+    if T > 1000:
+        D, L, O, k = 64, 8, 16, 16       # (narrow leaves, more than four pairs a leaf)
+    z = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(E)
+    x = torch.randn((T, D), generator=g, device="cuda").bfloat16()
+    b1 = torch.randn((E, L), generator=g, device="cuda").bfloat16()
+    b2 = torch.randn((E, O), generator=g, device="cuda").bfloat16()
+    idx = torch.randint(0, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    idx[3] = E - 1
+    weight = torch.rand((T, k), generator=g, device="cuda")
+    out = torch.full((T, O), -7.0, dtype=torch.bfloat16, device="cuda")
+    nb = R.blocks
+    F.fff_leaf_forward_mx4(x, z(E, L, 16 * nb(D)), z(E, L, nb(D)), b1, z(E, O, 16 * nb(L)), z(E, O, nb(L)), b2, idx, weight, F.ACT_RELU, out)
+    want = (weight.double()[:, :, None] * b2.double()[idx.long()]).sum(1).cpu().numpy()
+    size = (weight.double()[:, :, None] * b2.double()[idx.long()].abs()).sum(1).cpu().numpy()
+    # k products and sums in single precision, half a step of bf16
+    _within(out, want, 2 * k * 2.0 ** -24 * size + R.HALF["bf16"] * (np.abs(want) + 2 * k * 2.0 ** -24 * size), "biases")
+
+
 def test_leaves_all_tokens_in_one_of_many():
     import torch
     import paper_2308_14711_amd as F
@@ -462,6 +487,76 @@ def test_route_backward_ignores_indices_out_of_range_and_adds_repeated_ones():
         F.fff_moe_route_backward(logits, _bytes(idx), _bytes(count), d, dweight=_bytes(dw), normalise=normalise)
         want, size = R.route_backward(l, idx, count, dw, None, None, normalise)
         _within(d, want, 3 * _rtol(l, 12) * size + 1e-36, "dlogits")
+
+
+# ---- far offsets ---------------------------------------------------------------------------------------------
+
+
+def test_rows_beyond_four_gigabytes():
+    """Offsets that pass 32 bits: the last rows of large matrices, against the 64-bit forms of these rows."""
+    import torch
+    import paper_2308_14711_amd as F
+    n64 = lambda t: t.float().cpu().numpy().astype(np.float64)
+    u8 = lambda *s: torch.empty(s, dtype=torch.uint8, device="cuda")
+    rng = np.random.default_rng(4)
+    T, D, tail = 540000, 4100, 70
+    x = torch.empty((T, D), dtype=torch.bfloat16, device="cuda")         # 4.4 GB
+    for part in x.split(60000):
+        part.normal_()
+    nb = R.blocks(D)
+    codes, scales, back = u8(T, 16 * nb), u8(T, nb), torch.empty((T, D), dtype=torch.bfloat16, device="cuda")
+    F.fff_mx4_quantize(x, codes, scales)
+    F.fff_mx4_dequantize(codes, scales, back)
+    c, s = R.quantise(n64(x[-tail:]))
+    assert np.array_equal(codes[-tail:].cpu().numpy(), c) and np.array_equal(scales[-tail:].cpu().numpy(), s)
+    assert np.array_equal(n64(back[-tail:]), R.values(c, s, D))
+    del back
+    # products: codes, bf16 rows that are copied (4100 is no multiple of 8), and bf16 rows as they are
+    wc, ws, w = _matrix(rng, (40, D), D ** -0.5)
+    out = torch.empty((T, 40), dtype=torch.bfloat16, device="cuda")
+    F.fff_mx4_product(codes, _bytes(wc), _bytes(ws), out, a_scales=scales)
+    want, tol = R.product(R.values(c, s, D), w, None, "none", "bf16")
+    _within(out[-tail:], want, tol, "codes")
+    del codes, scales
+    F.fff_mx4_product(x, _bytes(wc), _bytes(ws), out)
+    want, tol = R.product(n64(x[-tail:]), w, None, "none", "bf16")
+    _within(out[-tail:], want, tol, "copied rows")
+    rows = x.view(-1)[:539000 * 4104].view(539000, 4104)
+    wc, ws, w = _matrix(rng, (40, 4104), 4104 ** -0.5)
+    F.fff_mx4_product(rows, _bytes(wc), _bytes(ws), out[:539000])
+    want, tol = R.product(n64(rows[-tail:]), w, None, "none", "bf16")
+    _within(out[539000 - tail:539000], want, tol, "rows as they are")
+    # leaves: tokens gathered from all over
+    T, D = rows.shape
+    c1, s1, w1 = _matrix(rng, (3, 32, D), D ** -0.5)
+    c2, s2, w2 = _matrix(rng, (3, 24, 32), 32 ** -0.5)
+    b1, b1v = _up(rng.normal(size=(3, 32)), "bf16")
+    b2, b2v = _up(rng.normal(size=(3, 24)), "bf16")
+    idx = torch.randint(0, 3, (T,), device="cuda", dtype=torch.int32)
+    y = torch.empty((T, 24), dtype=torch.bfloat16, device="cuda")
+    F.fff_leaf_forward_mx4(rows, _bytes(c1), _bytes(s1), b1, _bytes(c2), _bytes(s2), b2, idx, None, F.ACT_RELU, y)
+    for at in (slice(0, tail), slice(T - tail, T)):
+        want, tol = R.leaves(n64(rows[at]), w1, b1v, w2, b2v, idx[at].cpu().numpy()[:, None], None, "relu")
+        _within(y[at], want, tol, "leaves")
+    del x, rows
+    torch.cuda.empty_cache()
+    # routing: 2^31 and more elements
+    T, E, k = (1 << 22) + 5, 520, 2
+    logits = torch.empty((T, E), dtype=torch.bfloat16, device="cuda")
+    for part in logits.split(1 << 19):
+        part.normal_()
+    idx, weight, d = torch.empty((T, k), dtype=torch.int32, device="cuda"), torch.empty((T, k), device="cuda"), torch.empty_like(logits)
+    count = torch.empty((E + 1,), dtype=torch.int32, device="cuda")
+    F.fff_moe_route(logits, k, idx, weight, count)
+    assert int(count[E]) == T and int(count[:E].sum()) == T * k
+    dw = torch.randn((T, k), device="cuda")
+    F.fff_moe_route_backward(logits, idx, count, d, dweight=dw)
+    l = n64(logits[-tail:])
+    want = R.route(l, k)
+    assert np.array_equal(idx[-tail:].cpu().numpy(), want[0])
+    _within(weight[-tail:], want[1], _rtol(l, E) * want[1], "weight")
+    g, size = R.route_backward(l, want[0], count.cpu().numpy(), n64(dw[-tail:]), None)
+    _within(d[-tail:], g, 3 * _rtol(l, E) * size + R.HALF["bf16"] * np.abs(g) + 1e-36, "dlogits")
 
 
 # ---- together ----------------------------------------------------------------------------------------------
