@@ -1,4 +1,4 @@
-"""MI355X-native hard-routed inference of Fast Feedforward (FFF) layers.
+"""MI355X-native hard-routed inference of Fast Feedforward (FFF) layers, and operators for mixtures of experts and four-bit weights.
 
 The work is done by hand-written HIP kernels behind a C ABI (include/fff.h,
 built into libfff_hip.so).  This package is only the ctypes binding: it turns
