@@ -74,41 +74,43 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char* __restric
     }
 }
 
-// The transposed matrix: a block of threads takes 128 rows x 64 columns through LDS, then a thread one column's 32 rows.
+// The transposed matrix: 64 columns x 128 rows a block, a lane one column's 32 rows (read row by row, 64 columns of a row at once, all 32 on their way together),
+// a wave one block of 32 of each column.  The codes cross LDS so that a column's four blocks leave as 64 bytes in a piece.
 constexpr int kTransRows = 128, kTransCols = 64;
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const char* __restrict__ src, uint8_t* __restrict__ codes,
                                                                    uint8_t* __restrict__ scales, int64_t rows, int64_t cols,
                                                                    int64_t col_tiles, int64_t row_tiles) {
-    __shared__ float tile[kTransRows][kTransCols + 1];
+    __shared__ uint4 part[kTransCols * 5];         // four blocks of a column, five apart
+    __shared__ uint8_t part_s[kTransCols * 4];
     constexpr int es = BF16 ? 2 : 4;
     const int64_t nb = (rows + kMxBlock - 1) / kMxBlock;
     const int64_t per = col_tiles * row_tiles;
     const int64_t b = blockIdx.x / per, at = blockIdx.x - b * per;
-    const int64_t r0 = at / col_tiles * kTransRows, c0 = at % col_tiles * kTransCols;
+    const int64_t c0 = at % col_tiles * kTransCols, kb0 = at / col_tiles * (kTransRows / kMxBlock);
     src += b * rows * cols * es;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    // (addresses of elements behind the matrix: its first; sixteen loads a wave on their way at once)
-#pragma unroll 16
-    for (int r = wv; r < kTransRows; r += 4) {
-        const bool in = r0 + r < rows && c0 + lane < cols;
-        const float v = Elem<BF16>::load(src, in ? (r0 + r) * cols + c0 + lane : 0);
-        tile[r][lane] = in ? v : 0.0f;
+    const int64_t r0 = (kb0 + wv) * kMxBlock, c = c0 + lane < cols ? c0 + lane : cols - 1;
+    if (r0 < rows) {
+        float f[32];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) f[i] = Elem<BF16>::load(src, (r0 + i < rows ? r0 + i : rows - 1) * cols + c);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            f[i] = r0 + i < rows ? f[i] : 0.0f;
+            m = max(m, magnitude(f[i]));
+        }
+        const uint32_t s = scale_byte(m);
+        part[lane * 5 + wv] = make_uint4(pack_codes(f, s), pack_codes(f + 8, s), pack_codes(f + 16, s), pack_codes(f + 24, s));
+        part_s[lane * 4 + wv] = (uint8_t)s;
     }
     __syncthreads();
-    const int64_t c = c0 + (tid >> 2), kb = r0 / kMxBlock + (tid & 3);
-    if (c >= cols || kb >= nb) return;
-    float f[32];
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        f[i] = tile[(tid & 3) * 32 + i][tid >> 2];
-        m = max(m, magnitude(f[i]));
-    }
-    const uint32_t s = scale_byte(m);
-    const int64_t o = (b * cols + c) * nb + kb;
-    *(uint4*)(codes + o * 16) = make_uint4(pack_codes(f, s), pack_codes(f + 8, s), pack_codes(f + 16, s), pack_codes(f + 24, s));
-    scales[o] = (uint8_t)s;
+    const int64_t to = c0 + (tid >> 2), kb = kb0 + (tid & 3);
+    if (to >= cols || kb >= nb) return;
+    const int64_t o = (b * cols + to) * nb + kb;
+    *(uint4*)(codes + o * 16) = part[(tid >> 2) * 5 + (tid & 3)];
+    scales[o] = part_s[tid];
 }
 
 // Eight elements a lane, as in mx4_quantize_kernel.
