@@ -72,7 +72,9 @@ template <class T, class OP> __device__ __forceinline__ T group_reduce(T v, int 
     }
     return v;
 }
-__device__ __forceinline__ float group_max(float v, int G) { return group_reduce(v, G, [](float a, float b) { return fmaxf(a, b); }); }
+// the larger of two that are no NaN (fmaxf spends an instruction on making one quiet)
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, __builtin_inff()); }
+__device__ __forceinline__ float group_max(float v, int G) { return group_reduce(v, G, [](float a, float b) { return larger(a, b); }); }
 __device__ __forceinline__ float group_add(float v, int G) { return group_reduce(v, G, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ uint32_t group_max(uint32_t v, int G) { return group_reduce(v, G, [](uint32_t a, uint32_t b) { return max(a, b); }); }
 __device__ __forceinline__ int group_min(int v, int G) { return group_reduce(v, G, [](int a, int b) { return min(a, b); }); }
@@ -108,8 +110,8 @@ template <bool BF16, int V, bool VEC> struct RawRow {
             }
         }
     }
-    // its logits: -infinity for NaN, behind the row's end and in a row that takes no part; whether there are others
-    __device__ __forceinline__ bool values(const RouteArgs& a, bool there, int gi, float (&l)[V], float* largest) const {
+    // its logits: -infinity for NaN, behind the row's end and in a row that takes no part
+    __device__ __forceinline__ void values(const RouteArgs& a, bool there, int gi, float (&l)[V]) const {
         const float ninf = -__builtin_inff();
         const bool row_on = there && on;
         if constexpr (VEC) {
@@ -127,12 +129,6 @@ template <bool BF16, int V, bool VEC> struct RawRow {
                 l[v] = row_on && element<BF16, VEC>(v, gi, a.lanes) < a.E && l[v] == l[v] ? l[v] : ninf;
             }
         }
-        float m = ninf;
-#pragma unroll
-        for (int v = 0; v < V; ++v) m = fmaxf(m, l[v]);
-        m = group_max(m, a.lanes);
-        *largest = m;
-        return m > ninf;
     }
 };
 
@@ -154,72 +150,90 @@ template <int V> __device__ __forceinline__ void shares_of(const float (&l)[V], 
 // order of LDS accesses within a wave (they execute in order; the compiler must keep them so)
 __device__ __forceinline__ void wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// One by one the largest logits that a group holds; values of -infinity are none.
+// A value's bits in the order of values (-0 as 0), and back.  -infinity's are kNoKey.
+constexpr uint32_t kNoKey = 0x007fffffu;
+__device__ __forceinline__ uint32_t order_key(float v) {
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
+// One by one the largest logits that a group holds; values of -infinity are none.  Values are compared as keys, whole numbers: a maximum is one
+// instruction then (of floats two, the one before it making NaNs quiet).
 //
-// bf16 logits: value and index are one 32-bit key (the value's bits in the order of values, then the index turned round), so that the
-// largest key is the choice, ties included.  fp32: the lane whose largest value is the group's takes it from its registers; only where two
-// lanes hold it the lower index is looked for.
+// bf16 logits: value and index are one key, the index turned round in the low half, so that the largest key is the choice, ties included.  fp32: the lane
+// whose largest key is the group's takes it from its registers, those of the fours that hold it; only where two lanes hold it the lower index is looked for.
 template <bool BF16, int V, bool VEC> struct Picker {
-    float l[V];
-    uint32_t key[BF16 ? V : 1];
-    float mine;
+    uint32_t key[V];
+    uint32_t four[BF16 ? 1 : V / 4];      // the largest of four registers each
+    uint32_t mine;                        // of all
     __device__ __forceinline__ Picker(const float (&row)[V], int gi, int G) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            key[v] = order_key(row[v]);
+            if constexpr (BF16) key[v] = (key[v] & 0xffff0000u) | (0xffffu - (uint32_t)element<BF16, VEC>(v, gi, G));
+        }
+        mine = 0;
         if constexpr (BF16) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t b = __float_as_uint(row[v] + 0.0f);            // (-0 as 0)
-                const uint32_t up = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-                key[v] = (up & 0xffff0000u) | (0xffffu - (uint32_t)element<BF16, VEC>(v, gi, G));
-            }
+            for (int v = 0; v < V; ++v) mine = max(mine, key[v]);
         } else {
-            mine = -__builtin_inff();
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                l[v] = row[v];
-                mine = fmaxf(mine, l[v]);
+            for (int q = 0; q < V / 4; ++q) {
+                four[q] = max(max(key[4 * q], key[4 * q + 1]), max(key[4 * q + 2], key[4 * q + 3]));
+                mine = max(mine, four[q]);
             }
         }
     }
-    // Whether there is one; its value; `at`: its index, in the one lane that answers true.
+    // the largest value, before the first choice
+    __device__ __forceinline__ float largest(int G) const {
+        const uint32_t best = group_max(mine, G);
+        if constexpr (BF16) return best < 0x00800000u ? -__builtin_inff() : key_value((best & 0xffff0000u) | (best & 0x80000000u ? 0u : 0xffffu));
+        else return key_value(best);
+    }
+    // Whether there is one (`found`); its value; `at`: its index, in the one lane that answers true.
     __device__ __forceinline__ bool next(int gi, int G, float* value, int* at, bool* found) {
+        const uint32_t best = group_max(mine, G);
         if constexpr (BF16) {
-            uint32_t best = 0;
+            mine = 0;
 #pragma unroll
-            for (int v = 0; v < V; ++v) best = max(best, key[v]);
-            best = group_max(best, G);
-#pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0u : key[v];
+            for (int v = 0; v < V; ++v) {
+                key[v] = key[v] == best ? 0u : key[v];
+                mine = max(mine, key[v]);
+            }
             *found = best >= 0x00800000u;          // (above -infinity's 0x007f....)
             *at = 0xffff - (int)(best & 0xffffu);
-            const uint32_t up = best & 0xffff0000u;
-            *value = __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up & 0xffff0000u);
+            *value = key_value((best & 0xffff0000u) | (best & 0x80000000u ? 0u : 0xffffu));
             return gi == 0 && *found;
         } else {
-            const float ninf = -__builtin_inff();
-            const float best = group_max(mine, G);
-            *value = best;
-            *found = best > ninf;
+            *value = key_value(best);
+            *found = best > kNoKey;
             bool have = mine == best && *found;
             if (__popcll(__ballot(have)) != __popcll(__ballot(*found && gi == 0))) {     // two lanes hold it somewhere
                 int lowest = 0x7fffffff;
 #pragma unroll
                 for (int v = V - 1; v >= 0; --v)
-                    if (l[v] == best) lowest = element<BF16, VEC>(v, gi, G);
+                    if (key[v] == best) lowest = element<BF16, VEC>(v, gi, G);
                 const int first = group_min(have ? lowest : 0x7fffffff, G);       // (of all lanes)
                 have = have && lowest == first;
             }
-            if (have) {
-                bool taken = false;
-                mine = ninf;
+            bool open = have;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const bool hit = l[v] == best && !taken;
+            for (int q = 0; q < V / 4; ++q) {
+                const bool here = open && four[q] == best;
+                if (!__any(here)) continue;
+#pragma unroll
+                for (int v = 4 * q; v < 4 * q + 4; ++v) {
+                    const bool hit = open && key[v] == best;
                     *at = hit ? element<BF16, VEC>(v, gi, G) : *at;
-                    l[v] = hit ? ninf : l[v];
-                    taken = taken || hit;
-                    mine = fmaxf(mine, l[v]);
+                    key[v] = hit ? 0u : key[v];
+                    open = open && !hit;
                 }
+                four[q] = max(max(key[4 * q], key[4 * q + 1]), max(key[4 * q + 2], key[4 * q + 3]));
             }
+            mine = 0;
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) mine = max(mine, four[q]);
             return have;
         }
     }
@@ -255,9 +269,12 @@ __global__ __launch_bounds__(64 * route_waves(V, VEC)) void route_kernel(const R
     for (; t0 < a.T; t0 += step) {
         const int64_t t = t0 + lane / G;
         const bool there = t < a.T;
-        float l[V], m;
-        const bool any = raw.values(a, there, gi, l, &m);
+        float l[V];
+        raw.values(a, there, gi, l);
         if (t0 + step < a.T) raw.load(a, t + step, gi);
+        Picker<BF16, V, VEC> picker(l, gi, G);
+        const float m = picker.largest(G);
+        const bool any = m > -__builtin_inff();
         float total = 0;
         if (stats || !a.normalise) {
             float p[V];
@@ -276,7 +293,6 @@ __global__ __launch_bounds__(64 * route_waves(V, VEC)) void route_kernel(const R
                 }
             }
         }
-        Picker<BF16, V, VEC> picker(l, gi, G);
         for (int i = 0; i < k; ++i) {
             float value;
             int at = 0;
@@ -481,8 +497,12 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
                 slot_x[s] = Elem<BF16>::load(row, slot_e[s] < (uint32_t)E ? slot_e[s] : 0);
             }
         }
-        float l[V], d[V], m;
-        const bool any = raw.values(a, there, gi, l, &m);
+        float l[V], d[V], m = -__builtin_inff();
+        raw.values(a, there, gi, l);
+#pragma unroll
+        for (int v = 0; v < V; ++v) m = larger(m, l[v]);
+        m = group_max(m, G);
+        const bool any = m > -__builtin_inff();
         if (t0 + step < a.T) ask(t + step);
         float s = 0, dot = 0;
         shares_of(l, m, any, d);

@@ -338,15 +338,17 @@ template <bool A4, int MT> struct TileShape {
 };
 
 template <bool A4, int MODE, bool WIDE, int MT>
-__global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a, const uint32_t row_tiles, const uint32_t col_tiles) {
+__global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a, const uint32_t max_row_tiles, const uint32_t col_tiles) {
     typedef TileShape<A4, MT> S;
     constexpr int NT = S::NT;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
     // an XCD takes a contiguous range of tiles, kGroup row tiles against all columns at a time
     constexpr uint32_t kGroup = 4;
-    const uint32_t id = (blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;
-    if (id >= row_tiles * col_tiles) return;
+    // (of the tiles that there are: a grid for the most that leaves can have leaves one XCD a part of its range)
+    const uint32_t row_tiles = MODE == kDense ? max_row_tiles : (uint32_t)*a.n_tiles;
+    const uint32_t share = (row_tiles * col_tiles + kXcds - 1) / kXcds, id = (blockIdx.x % kXcds) * share + blockIdx.x / kXcds;
+    if (blockIdx.x / kXcds >= share || id >= row_tiles * col_tiles) return;
     const uint32_t group = id / (kGroup * col_tiles), in = id - group * kGroup * col_tiles;
     const uint32_t tall = row_tiles - kGroup * group < kGroup ? row_tiles - kGroup * group : kGroup;
     const int64_t rt = kGroup * group + in % tall, ct = in / tall;
@@ -356,7 +358,6 @@ __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a,
         first = rt * S::kRows;
         rows = a.T - first;
     } else {
-        if (rt >= *a.n_tiles) return;
         leaf = a.tile_leaf[rt];
         first = a.tile_slot[rt];
         rows = a.start[leaf + 1] - first;
