@@ -1,12 +1,14 @@
 // Choice of k experts per token from gating logits, their mixture weights, per-expert counts and balance losses, and the gradient.
 //
 // One pass over the logits: a group of G lanes (a power of two) holds a token's row in V registers a lane, takes its maximum and
-// sum of exponentials, and picks the k largest one after another (the maximum over the group, then the lowest index that holds it).  What the
+// sum of exponentials, and picks the k largest: one after another (the maximum over the group, then the lowest index that holds it), or where k is
+// larger all at once (the few that reach a bound below the k-th, each of which counts those before it).  What the
 // losses need of all tokens -- sum over tokens of p, the counts, sum of lse^2 -- stays in registers and LDS over the tokens of a block
 // and leaves as one row per block; a second launch adds the rows of the blocks up, always in the same order.
 // The gradient is one pass as well: with c[e] = dloss[0] E f[e] / n, p and lse from the logits again,
 //   dlogits[e] = p[e] (c[e] - sum_j c[j] p[j] + 2 dloss[1] lse / n) + the weights' part on the k chosen.
-// Both are bound by the bytes of the logits (and their gradient).
+// The gradient is bound by the bytes of the logits and their gradient (32768 x 512 fp32, 201 MB in all with the forward pass: 31 us, 4.2 TB/s), the
+// forward pass by its instructions (29 us there, two thirds of them in the choice of 8, the exponentials and the sums; bytes alone would take 13).
 #include "fff_device.h"
 #include "fff_mx4.h"
 
@@ -16,7 +18,7 @@ namespace {
 constexpr int kBackwardWaves = 4;
 constexpr int kMaxBackwardBlocks = 2048;
 // Waves of a block of the forward kernel: as many as its sums of p per wave leave room for in LDS and its registers on a compute unit, since a
-// block leaves one row of partial sums (sixteen waves a block on 256 blocks instead of four on 512, 512 experts: 92 -> 45 us).
+// block leaves one row of partial sums (sixteen waves a block on 256 blocks instead of four on 512, 512 experts: 92 -> 70 us).
 constexpr int route_waves(int V, bool pieces) { return V == 8 ? 16 : V == 16 ? (pieces ? 16 : 8) : 4; }
 
 struct RouteArgs {
@@ -36,6 +38,7 @@ struct RouteArgs {
     int64_t T;
     int E, k, lanes;             // lanes: G
     bool normalise;
+    bool at_once;                // forward: the k choices together (Picker::all)
 };
 
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
@@ -163,6 +166,10 @@ __device__ __forceinline__ float key_value(uint32_t key) { return __uint_as_floa
 //
 // bf16 logits: value and index are one key, the index turned round in the low half, so that the largest key is the choice, ties included.  fp32: the lane
 // whose largest key is the group's takes it from its registers, those of the fours that hold it; only where two lanes hold it the lower index is looked for.
+// (32768 rows of 512 in fp32, 8 one by one: 46 us with floats, 41 with keys.)
+// of a bf16 logit's key, whose low half is not its own
+__device__ __forceinline__ float short_value(uint32_t key) { return key_value((key & 0xffff0000u) | (key & 0x80000000u ? 0u : 0xffffu)); }
+constexpr int kReached = 64;
 template <bool BF16, int V, bool VEC> struct Picker {
     uint32_t key[V];
     uint32_t four[BF16 ? 1 : V / 4];      // the largest of four registers each
@@ -174,22 +181,82 @@ template <bool BF16, int V, bool VEC> struct Picker {
             if constexpr (BF16) key[v] = (key[v] & 0xffff0000u) | (0xffffu - (uint32_t)element<BF16, VEC>(v, gi, G));
         }
         mine = 0;
-        if constexpr (BF16) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) mine = max(mine, key[v]);
-        } else {
+        for (int v = 0; v < V; ++v) mine = max(mine, key[v]);
+    }
+    // before the first of next()
+    __device__ __forceinline__ void start() {
+        if constexpr (!BF16) {
 #pragma unroll
-            for (int q = 0; q < V / 4; ++q) {
-                four[q] = max(max(key[4 * q], key[4 * q + 1]), max(key[4 * q + 2], key[4 * q + 3]));
-                mine = max(mine, four[q]);
-            }
+            for (int q = 0; q < V / 4; ++q) four[q] = max(max(key[4 * q], key[4 * q + 1]), max(key[4 * q + 2], key[4 * q + 3]));
         }
     }
     // the largest value, before the first choice
     __device__ __forceinline__ float largest(int G) const {
         const uint32_t best = group_max(mine, G);
-        if constexpr (BF16) return best < 0x00800000u ? -__builtin_inff() : key_value((best & 0xffff0000u) | (best & 0x80000000u ? 0u : 0xffffu));
+        if constexpr (BF16) return best < 0x00800000u ? -__builtin_inff() : short_value(best);
         else return key_value(best);
+    }
+    // All k choices at once (16 lanes or more): the k-th largest of the lanes' largest is no more than the k-th choice, and few logits reach
+    // it (512 of 32 lanes, k = 8: 9).  Those meet in LDS, a lane counts how many of them come before its own, and that is its slot.  False, with nothing
+    // done, where a row of the wave has more than kReached of them.
+    __device__ __forceinline__ bool all(int k, int gi, int G, uint64_t* reached, float* slot_value, int* slot_at, int32_t* counts) const {
+        asm volatile("" : "+v"(gi));       // (indexes are formed where they are used, not kept in registers over the rows)
+        uint32_t left = mine, bound = 0;
+        for (int i = 0; i < k; ++i) {
+            bound = group_max(left, G);
+            left = left == bound ? 0u : left;
+        }
+        bound = max(bound, BF16 ? 0x00800000u : kNoKey + 1);
+        int own = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) own += key[v] >= bound;
+        // its place behind those of the lanes before it
+        int upto = own;
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, true);         // from one, two, four, eight lanes before, in sixteen
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, true);
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, true);
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, true);
+        if (G >= 32) upto += __builtin_amdgcn_update_dpp(0, upto, 0x142, 0xa, 0xf, false);        // sixteen's last to the next sixteen
+        if (G == 64) upto += __builtin_amdgcn_update_dpp(0, upto, 0x143, 0xc, 0xf, false);
+        const int n1 = __builtin_amdgcn_readlane(upto, 63);
+        int n = n1, most = n1;
+        if (G < 64) {
+            const int n0 = __builtin_amdgcn_readlane(upto, 31);
+            n = threadIdx.x & 32 ? n1 : n0;
+            most = max(n0, n1);
+        }
+        if (G < 32) {
+            const int n0 = __builtin_amdgcn_readlane(upto, 15), n2 = __builtin_amdgcn_readlane(upto, 47);
+            n = threadIdx.x & 16 ? n : threadIdx.x & 32 ? n2 : n0;
+            most = max(most, max(n0, n2));
+        }
+        if (most > kReached) return false;
+        const int end = (most + 3) & ~3;
+        for (int i = gi; i < end; i += G) reached[i] = 0;
+        wave_sync();
+        uint64_t* to = reached + (upto - own);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (key[v] >= bound) *to++ = (uint64_t)key[v] << 32 | (BF16 ? 0u : (uint32_t)~element<BF16, VEC>(v, gi, G));
+        wave_sync();
+        for (int c = gi; c < end; c += G) {
+            const uint64_t x = reached[c];
+            int before = 0;
+            for (int i = 0; i < end; i += 4) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) before += reached[i + u] > x;
+            }
+            if (c < n && before < k) {
+                const uint32_t high = (uint32_t)(x >> 32);
+                const int at = BF16 ? 0xffff - (int)(high & 0xffffu) : (int)~(uint32_t)x;
+                slot_value[before] = BF16 ? short_value(high) : key_value(high);
+                slot_at[before] = at;
+                if (counts) atomicAdd(counts + at, 1);
+            }
+        }
+        for (int i = n + gi; i < k; i += G) slot_at[i] = -1;
+        return true;
     }
     // Whether there is one (`found`); its value; `at`: its index, in the one lane that answers true.
     __device__ __forceinline__ bool next(int gi, int G, float* value, int* at, bool* found) {
@@ -203,12 +270,13 @@ template <bool BF16, int V, bool VEC> struct Picker {
             }
             *found = best >= 0x00800000u;          // (above -infinity's 0x007f....)
             *at = 0xffff - (int)(best & 0xffffu);
-            *value = key_value((best & 0xffff0000u) | (best & 0x80000000u ? 0u : 0xffffu));
+            *value = short_value(best);
             return gi == 0 && *found;
         } else {
             *value = key_value(best);
             *found = best > kNoKey;
             bool have = mine == best && *found;
+            asm volatile("" : "+v"(gi));       // (as above)
             if (__popcll(__ballot(have)) != __popcll(__ballot(*found && gi == 0))) {     // two lanes hold it somewhere
                 int lowest = 0x7fffffff;
 #pragma unroll
@@ -251,7 +319,8 @@ __global__ __launch_bounds__(64 * route_waves(V, VEC)) void route_kernel(const R
     const int slots = kWaves * rows * k;
     float* const my_w = lds + (tid / G) * k;
     int32_t* const my_i = (int32_t*)lds + slots + (tid / G) * k;
-    float* const sums = lds + 2 * slots;
+    uint64_t* const reached = (uint64_t*)(lds + 2 * slots) + tid / G * kReached;
+    float* const sums = lds + 2 * slots + (a.at_once ? 2 * kWaves * rows * kReached : 0);
     int32_t* const counts = (int32_t*)sums + kWaves * E;
     float acc[V], z = 0;
     int n = 0;
@@ -293,7 +362,9 @@ __global__ __launch_bounds__(64 * route_waves(V, VEC)) void route_kernel(const R
                 }
             }
         }
-        for (int i = 0; i < k; ++i) {
+        const bool done = a.at_once && picker.all(k, gi, G, reached, my_w, my_i, stats ? counts : nullptr);
+        if (!done) picker.start();
+        for (int i = done ? k : 0; i < k; ++i) {
             float value;
             int at = 0;
             bool found;
@@ -573,15 +644,16 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
     }
 }
 
-// Registers a lane (a power of two, 8 at least) and lanes a row.  A row on fewer lanes shares the steps over the lanes among more rows of a wave
-// (512 fp32 logits, 8 chosen: half a wave, 16 registers a lane).
-void route_shape(int64_t E, int* V, int* G) {
-    *V = E <= 256 ? 8 : E <= 1024 ? 16 : E <= 2048 ? 32 : 64;
+// Registers a lane (a power of two, 8 at least) and lanes a row.  A row on fewer lanes shares the steps over the lanes among more rows of a wave, in the
+// forward kernel also those of the choices, so that eight registers end at 64 experts there (65536 rows, forward and finish: 256 bf16 logits, k = 2 and 8,
+// 30.1 and 39.6 us with eight, 23.5 and 30.4 with sixteen; 128: 19.2 and 25.0, 17.0 and 22.3; fp32 128, k = 8: 25.3, and 31.0 since eight lanes do not
+// choose at once) and at 256 in the backward kernel (256 bf16 logits: 28.5, sixteen 32.3).
+void route_shape(int64_t E, int64_t up_to_8, int* V, int* G) {
+    *V = E <= up_to_8 ? 8 : E <= 1024 ? 16 : E <= 2048 ? 32 : 64;
     int g = 1;
     while (g * *V < E) g *= 2;
     *G = g;
 }
-
 // Rows of partial sums that scratch has room for, and blocks of the forward kernel: one a compute unit (50432 tokens, 128 experts: 14.7 us; two: 17.4).
 constexpr int64_t kMaxPartRows = 256;
 int route_blocks(int64_t T, int waves, int G) {
@@ -624,7 +696,7 @@ struct RouteScratch {
     }
 };
 
-RouteArgs common_args(const Route& r, int* V, bool* vec) {
+RouteArgs common_args(const Route& r, int64_t up_to_8, int* V, bool* vec) {
     RouteArgs a{};
     a.logits = r.logits;
     a.mask = r.mask;
@@ -632,7 +704,7 @@ RouteArgs common_args(const Route& r, int* V, bool* vec) {
     a.E = (int)r.E;
     a.k = r.k;
     a.normalise = r.normalise;
-    route_shape(r.E, V, &a.lanes);
+    route_shape(r.E, up_to_8, V, &a.lanes);
     *vec = vec_ok(r.logits, r.E, r.bf16);
     return a;
 }
@@ -652,7 +724,11 @@ hipError_t launch_route(const Route& r, int32_t* idx, float* weight, int32_t* co
     }
     int V;
     bool vec;
-    RouteArgs a = common_args(r, &V, &vec);
+    // Choices one by one or at once (65536 rows of 256, us, one by one / at once: bf16 k = 2 30 / 33, 4 35 / 36, 8 45 / 41; fp32 k = 2 33 / 33, 4 41 / 35,
+    // 8 60 / 40; 32768 fp32 rows of 512, k = 8: 45 / 33).  With k near the lanes' number too many logits reach the bound.
+    const int late = r.bf16 ? 6 : 3;
+    RouteArgs a = common_args(r, !r.bf16 && r.k >= late ? 128 : 64, &V, &vec);
+    a.at_once = a.lanes >= 16 && r.k >= late && 4 * r.k <= 3 * a.lanes;
     a.idx = idx;
     a.weight = weight;
     const RouteScratch at(r.T, r.E);
@@ -665,7 +741,7 @@ hipError_t launch_route(const Route& r, int32_t* idx, float* weight, int32_t* co
         a.ticket = (int32_t*)(base + at.ticket);
     }
     const int waves = route_waves(V, vec), blocks = route_blocks(r.T, waves, a.lanes);
-    const size_t lds = (size_t)waves * (64 / a.lanes) * r.k * 8 + (stats ? (size_t)(waves + 1) * r.E * 4 : 0);
+    const size_t lds = (size_t)waves * (64 / a.lanes) * 8 * (r.k + (a.at_once ? kReached : 0)) + (stats ? (size_t)(waves + 1) * r.E * 4 : 0);
     note_launch("route_kernel<%s,%d,%s>", r.bf16 ? "bf16" : "f32", V, vec ? "pieces" : "elements");
     hipError_t e = with_shape(r.bf16, V, vec, [&](auto B, auto N, auto X) {
         const auto kernel = route_kernel<decltype(B)::value, decltype(N)::value, decltype(X)::value>;
@@ -687,7 +763,7 @@ hipError_t launch_route_backward(const Route& r, const int32_t* idx, const int32
                                  void* dlogits, hipStream_t s) {
     int V;
     bool vec;
-    RouteArgs a = common_args(r, &V, &vec);
+    RouteArgs a = common_args(r, 256, &V, &vec);
     vec = vec && vec_ok(dlogits, r.E, r.bf16);
     a.idx = const_cast<int32_t*>(idx);
     a.count = count;

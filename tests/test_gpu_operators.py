@@ -445,6 +445,40 @@ def test_route_backward(case, parts):
     assert not got[~R.route(l, 1, mask)[7]].any() and not got[np.isnan(l) | (l == -np.inf)].any()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("E,k", [(65, 3), (128, 6), (129, 12), (250, 7), (256, 32), (260, 24), (512, 8), (700, 25), (1024, 31), (1300, 6), (2048, 32), (4096, 20)])
+def test_route_chooses_among_few_and_many_that_are_equal(E, k, kind):
+    """Rows with any number of finite logits, all of them equal or all but a few: whether choices are taken one by one or at once, ties
+    go to the lower index."""
+    import torch
+    import paper_2308_14711_amd as F
+    rng = np.random.default_rng(E * k)
+    there = [0, 1, 2, k - 1, k, k + 1, 31, 32, 33, 60, 63, 64, 65, 66, 80, E - 1, E]
+    T = 4 * len(there)
+    l = np.full((T, E), -np.inf)
+    for t in range(T):
+        n = min(there[t // 4], E)
+        at = rng.permutation(E)[:n]
+        l[t, at] = rng.normal() * 4                       # one value for all
+        if t % 4 == 1:
+            l[t, at] = rng.normal(size=n)
+        if t % 4 == 2:
+            l[t, at[: n // 2]] += 1.0                     # two
+        if t % 4 == 3:
+            few = at[: min(n, k - 1)]
+            l[t, few] += rng.integers(1, 4, len(few))     # fewer above than are to be chosen
+    order = rng.permutation(T)                            # rows of all kinds share a wave
+    logits, l = _up(l[order], kind)
+    idx, w = torch.empty((T, k), dtype=torch.int32, device="cuda"), torch.empty((T, k), device="cuda")
+    count = torch.empty((E + 1,), dtype=torch.int32, device="cuda")
+    want = R.route(l, k)
+    for stats in (None, count):
+        F.fff_moe_route(logits, k, idx, w, stats)
+        assert np.array_equal(idx.cpu().numpy(), want[0])
+        _within(w, want[1], _rtol(l, E) * want[1] + 1e-37, "weight")
+    assert np.array_equal(count.cpu().numpy(), want[2])
+
+
 def test_route_logits_of_plus_infinity_share_the_token():
     import torch
     import paper_2308_14711_amd as F
