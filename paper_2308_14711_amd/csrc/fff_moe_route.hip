@@ -17,9 +17,9 @@ namespace {
 
 constexpr int kBackwardWaves = 4;
 constexpr int kMaxBackwardBlocks = 2048;
-// Waves of a block of the forward kernel: as many as its sums of p per wave leave room for in LDS and its registers on a compute unit, since a
+// Waves of a block of the forward kernel: as many as its registers leave room for on a compute unit, since a
 // block leaves one row of partial sums (sixteen waves a block on 256 blocks instead of four on 512, 512 experts: 92 -> 70 us).
-constexpr int route_waves(int V, bool pieces) { return V == 8 ? 16 : V == 16 ? (pieces ? 16 : 8) : 4; }
+constexpr int route_waves(int V) { return V <= 16 ? 16 : V == 32 ? 8 : 4; }
 
 struct RouteArgs {
     const void* logits;
@@ -308,13 +308,14 @@ template <bool BF16, int V, bool VEC> struct Picker {
 };
 
 template <bool BF16, int V, bool VEC>
-__global__ __launch_bounds__(64 * route_waves(V, VEC)) void route_kernel(const RouteArgs a) {
-    constexpr int kWaves = route_waves(V, VEC);
+__global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteArgs a) {
+    constexpr int kWaves = route_waves(V);
     extern __shared__ float lds[];               // the slots chosen; statistics: kWaves x E sums, E counts
     __shared__ float block_z[kWaves];
     __shared__ int32_t block_n[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int G = a.lanes, gi = lane & (G - 1), rows = 64 / G, E = a.E, k = a.k;
+    const int G = a.lanes, rows = 64 / G, E = a.E, k = a.k;
+    int gi = lane & (G - 1);
     const bool stats = a.part_p != nullptr;
     const int slots = kWaves * rows * k;
     float* const my_w = lds + (tid / G) * k;
@@ -336,6 +337,7 @@ __global__ __launch_bounds__(64 * route_waves(V, VEC)) void route_kernel(const R
     if (t0 < a.T) raw.load(a, t0 + lane / G, gi);
     // (rows past the end and masked ones run along as empty rows: the lanes of a wave stay together)
     for (; t0 < a.T; t0 += step) {
+        if constexpr (V >= 16) asm volatile("" : "+v"(gi));        // (indexes are formed where they are used: kept over the rows they take registers)
         const int64_t t = t0 + lane / G;
         const bool there = t < a.T;
         float l[V];
@@ -514,7 +516,8 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
     extern __shared__ float patches[];           // G V words a group, zeros between rows
     constexpr int VE = BF16 ? 8 : 4, es = BF16 ? 2 : 4;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int G = a.lanes, gi = lane & (G - 1), rows = 64 / G, E = a.E, k = a.k;
+    const int G = a.lanes, rows = 64 / G, E = a.E, k = a.k;
+    int gi = lane & (G - 1);
     // a row's logits, chosen experts and their gradients, asked for ahead of their use
     int64_t t0 = ((int64_t)blockIdx.x * kBackwardWaves + wv) * rows;
     RawRow<BF16, V, VEC> raw;
@@ -553,6 +556,7 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void route_backward_kernel(con
     }
     const int64_t step = (int64_t)gridDim.x * kBackwardWaves * rows;
     for (; t0 < a.T; t0 += step) {
+        if constexpr (V >= 16) asm volatile("" : "+v"(gi));        // (indexes are formed where they are used: kept over the rows they take registers)
         const int64_t t = t0 + lane / G;
         const bool there = t < a.T;
         const int64_t tt = there ? t : a.T - 1;
@@ -740,7 +744,7 @@ hipError_t launch_route(const Route& r, int32_t* idx, float* weight, int32_t* co
         a.part_n = (int32_t*)(base + at.part_n);
         a.ticket = (int32_t*)(base + at.ticket);
     }
-    const int waves = route_waves(V, vec), blocks = route_blocks(r.T, waves, a.lanes);
+    const int waves = route_waves(V), blocks = route_blocks(r.T, waves, a.lanes);
     const size_t lds = (size_t)waves * (64 / a.lanes) * 8 * (r.k + (a.at_once ? kReached : 0)) + (stats ? (size_t)(waves + 1) * r.E * 4 : 0);
     note_launch("route_kernel<%s,%d,%s>", r.bf16 ? "bf16" : "f32", V, vec ? "pieces" : "elements");
     hipError_t e = with_shape(r.bf16, V, vec, [&](auto B, auto N, auto X) {
