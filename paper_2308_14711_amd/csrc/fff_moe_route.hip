@@ -38,7 +38,6 @@ struct RouteArgs {
     int64_t T;
     int E, k, lanes;             // lanes: G
     bool normalise;
-    bool at_once;                // forward: the k choices together (Picker::all)
 };
 
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
@@ -307,7 +306,7 @@ template <bool BF16, int V, bool VEC> struct Picker {
     }
 };
 
-template <bool BF16, int V, bool VEC>
+template <bool BF16, int V, bool VEC, bool ONCE>
 __global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteArgs a) {
     constexpr int kWaves = route_waves(V);
     extern __shared__ float lds[];               // the slots chosen; statistics: kWaves x E sums, E counts
@@ -321,7 +320,7 @@ __global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteA
     float* const my_w = lds + (tid / G) * k;
     int32_t* const my_i = (int32_t*)lds + slots + (tid / G) * k;
     uint64_t* const reached = (uint64_t*)(lds + 2 * slots) + tid / G * kReached;
-    float* const sums = lds + 2 * slots + (a.at_once ? 2 * kWaves * rows * kReached : 0);
+    float* const sums = lds + 2 * slots + (ONCE ? 2 * kWaves * rows * kReached : 0);
     int32_t* const counts = (int32_t*)sums + kWaves * E;
     float acc[V], z = 0;
     int n = 0;
@@ -364,7 +363,8 @@ __global__ __launch_bounds__(64 * route_waves(V)) void route_kernel(const RouteA
                 }
             }
         }
-        const bool done = a.at_once && picker.all(k, gi, G, reached, my_w, my_i, stats ? counts : nullptr);
+        bool done = false;
+        if constexpr (ONCE) done = picker.all(k, gi, G, reached, my_w, my_i, stats ? counts : nullptr);
         if (!done) picker.start();
         for (int i = done ? k : 0; i < k; ++i) {
             float value;
@@ -732,7 +732,7 @@ hipError_t launch_route(const Route& r, int32_t* idx, float* weight, int32_t* co
     // 8 60 / 40; 32768 fp32 rows of 512, k = 8: 45 / 33).  With k near the lanes' number too many logits reach the bound.
     const int late = r.bf16 ? 6 : 3;
     RouteArgs a = common_args(r, !r.bf16 && r.k >= late ? 128 : 64, &V, &vec);
-    a.at_once = a.lanes >= 16 && r.k >= late && 4 * r.k <= 3 * a.lanes;
+    const bool at_once = a.lanes >= 16 && r.k >= late && 4 * r.k <= 3 * a.lanes;
     a.idx = idx;
     a.weight = weight;
     const RouteScratch at(r.T, r.E);
@@ -745,10 +745,12 @@ hipError_t launch_route(const Route& r, int32_t* idx, float* weight, int32_t* co
         a.ticket = (int32_t*)(base + at.ticket);
     }
     const int waves = route_waves(V), blocks = route_blocks(r.T, waves, a.lanes);
-    const size_t lds = (size_t)waves * (64 / a.lanes) * 8 * (r.k + (a.at_once ? kReached : 0)) + (stats ? (size_t)(waves + 1) * r.E * 4 : 0);
+    const size_t lds = (size_t)waves * (64 / a.lanes) * 8 * (r.k + (at_once ? kReached : 0)) + (stats ? (size_t)(waves + 1) * r.E * 4 : 0);
     note_launch("route_kernel<%s,%d,%s>", r.bf16 ? "bf16" : "f32", V, vec ? "pieces" : "elements");
     hipError_t e = with_shape(r.bf16, V, vec, [&](auto B, auto N, auto X) {
-        const auto kernel = route_kernel<decltype(B)::value, decltype(N)::value, decltype(X)::value>;
+        constexpr bool bf16 = decltype(B)::value, pieces = decltype(X)::value;
+        constexpr int regs = decltype(N)::value;
+        const auto kernel = at_once ? route_kernel<bf16, regs, pieces, true> : route_kernel<bf16, regs, pieces, false>;
         if (lds > 60 * 1024) {
             const hipError_t rc = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (rc != hipSuccess) return rc;
