@@ -259,11 +259,12 @@ int fff_moe_route_backward(const void* logits, const uint8_t* token_mask, int64_
  *   src        [batch, rows, cols], dtype FFF_F32 or FFF_BF16
  *   transpose  0: codes and scales of the rows, [batch, rows, ...]; else of the columns, [batch, cols, ...] with blocks
  *              along `rows` (leaf_w2 [leaves, leaf_width, O] for fff_leaf_forward_mx4)
- * Errors: FFF_ERR_NULL, FFF_ERR_SHAPE (rows or cols < 1, or more than 2^40 elements), FFF_ERR_RANGE (batch < 0),
+ * Errors: FFF_ERR_NULL, FFF_ERR_SHAPE (rows or cols < 1, more than 2^40 elements, blocks counted whole, rows of more than 2^34, with
+ * transpose 2^24 tiles of 128 x 64 or more), FFF_ERR_RANGE (batch < 0),
  * FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (codes misaligned), FFF_ERR_ALIAS (codes or scales overlap src or each other), FFF_ERR_DEVICE.
  * batch == 0 is FFF_OK.
  *
- * fff_mx4_dequantize: the values, [rows, cols] of `dtype` (exact in both).
+ * fff_mx4_dequantize: the values, [rows, cols] of `dtype` (exact in both); the same errors, FFF_ERR_RANGE for rows < 0.
  */
 int fff_mx4_quantize(const void* src, uint8_t* codes, uint8_t* scales, int transpose, void* stream,
                      int64_t batch, int64_t rows, int64_t cols, int dtype);
@@ -280,7 +281,7 @@ int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, v
  *   scratch   device memory, 256-byte aligned, of one call until its launches have run, at least
  *             fff_mx4_product_scratch_bytes: a copy of bf16 rows that are not whole aligned pieces of 16 bytes (K not a
  *             multiple of 8, or a misaligned); never read otherwise, and may be NULL then
- * K <= 2^22, N <= 2^22.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T), FFF_ERR_SHAPE, FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (act, or misaligned codes),
+ * K <= 2^22, N <= 2^22, fewer than 2^24 tiles of 128 x 128 results (else FFF_ERR_SHAPE).  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T), FFF_ERR_SHAPE, FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (act, or misaligned codes),
  * FFF_ERR_ALIAS (out or scratch overlaps an input or each other), FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.
  */
 int fff_mx4_product(const void* a, const uint8_t* a_scales, const uint8_t* w, const uint8_t* w_scales,
@@ -301,7 +302,8 @@ size_t fff_mx4_product_scratch_bytes(int64_t T, int64_t K);
  *   scratch  device memory, 256-byte aligned, of one call until its launches have run, at least
  *            fff_leaf_mx4_scratch_bytes of the same sizes; needs no initial value
  * Hidden activations are rounded to bf16 (the operand type of the matrix cores), sums are fp32.  Results do not depend on the
- * order in which tokens are grouped.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T, k, n_leaves, leaf_width), FFF_ERR_SHAPE, FFF_ERR_DTYPE,
+ * order in which tokens are grouped.  D and O <= 2^22, and fewer than 2^24 tiles of 64 tokens x 128 columns (a part of one for every leaf;
+ * else FFF_ERR_SHAPE).  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T, k, n_leaves, leaf_width), FFF_ERR_SHAPE, FFF_ERR_DTYPE,
  * FFF_ERR_UNSUPPORTED, FFF_ERR_ALIAS, FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.
  */
 int fff_leaf_forward_mx4(const void* x, const uint8_t* leaf_w1, const uint8_t* leaf_s1, const void* leaf_b1,

@@ -1163,7 +1163,7 @@ int fff_mx4_quantize(const void* src, uint8_t* codes, uint8_t* scales, int trans
     if (batch == 0) return FFF_OK;
     // (blocks of 32 and tiles of columns count whole: 2^40 of either is the limit too)
     if (batch > kMaxElems / (rows * cols) || batch * (transpose ? cols : rows) > (kMaxElems >> 5) / mx_blocks(transpose ? rows : cols)) return FFF_ERR_SHAPE;
-    if (transpose && batch > (((int64_t)1 << 31) - 1) / (((rows + 127) / 128) * ((cols + 63) / 64))) return FFF_ERR_SHAPE;
+    if (transpose ? batch >= kMaxMx4Blocks / (((rows + 127) / 128) * ((cols + 63) / 64)) : cols > kMaxMx4Row) return FFF_ERR_SHAPE;
     if (!src || !codes || !scales) return FFF_ERR_NULL;
     if (!aligned16(codes)) return FFF_ERR_UNSUPPORTED;
     const int64_t blocks = batch * (transpose ? cols * mx_blocks(rows) : rows * mx_blocks(cols));
@@ -1177,7 +1177,7 @@ int fff_mx4_quantize(const void* src, uint8_t* codes, uint8_t* scales, int trans
 int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, void* stream, int64_t rows, int64_t cols, int dtype) {
     if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
     if (rows < 0 || rows > kMaxElems) return FFF_ERR_RANGE;
-    if (cols < 1 || cols > kMaxElems || (rows > 0 && mx_blocks(cols) > (kMaxElems >> 5) / rows)) return FFF_ERR_SHAPE;
+    if (cols < 1 || cols > kMaxMx4Row || (rows > 0 && mx_blocks(cols) > (kMaxElems >> 5) / rows)) return FFF_ERR_SHAPE;
     if (rows == 0) return FFF_OK;
     if (!codes || !scales || !out) return FFF_ERR_NULL;
     if (!aligned16(codes)) return FFF_ERR_UNSUPPORTED;
@@ -1199,7 +1199,7 @@ int fff_mx4_product(const void* a, const uint8_t* a_scales, const uint8_t* w, co
     if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
     if (T < 0 || T > kMaxTokens) return FFF_ERR_RANGE;
     if (K < 1 || N < 1 || K > kMaxMx4Side || N > kMaxMx4Side || T * mx_blocks(K) > (kMaxElems >> 5) || T * N > kMaxElems ||
-        N * mx_blocks(K) > (kMaxElems >> 5))
+        N * mx_blocks(K) > (kMaxElems >> 5) || ((T + 127) / 128) * ((N + 127) / 128) >= kMaxMx4Blocks)
         return FFF_ERR_SHAPE;
     if (act != FFF_ACT_RELU && act != FFF_ACT_GELU && act != FFF_ACT_NONE) return FFF_ERR_UNSUPPORTED;
     if (!a_scales && dtype != FFF_BF16) return FFF_ERR_UNSUPPORTED;
@@ -1241,6 +1241,8 @@ static int check_leaf_mx4(int64_t T, int64_t D, int64_t O, int64_t n_leaves, int
     const int64_t rows = T * k > n_leaves ? T * k : n_leaves;
     const int64_t m = (D > O ? D : O) + kMxBlock, l = leaf_width + kMxBlock;
     if (m > kMaxElems / rows || l > kMaxElems / rows || n_leaves * l > kMaxElems / m) return FFF_ERR_SHAPE;
+    const int64_t met = T * k < n_leaves ? T * k : n_leaves, columns = O > leaf_width ? O : leaf_width;
+    if ((T * k / 64 + met) * ((columns + 127) / 128) >= kMaxMx4Blocks) return FFF_ERR_SHAPE;
     return FFF_OK;
 }
 

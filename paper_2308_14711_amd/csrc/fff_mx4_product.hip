@@ -580,7 +580,6 @@ template <bool A4, int MODE, int MT> hipError_t launch_tiles(Args a, int64_t row
     typedef TileShape<A4, MT> S;
     const int64_t col_tiles = ((MODE == kHidden ? a.out_row : a.N) + S::kCols - 1) / S::kCols;
     const int64_t blocks = (row_tiles * col_tiles + kXcds - 1) / kXcds * kXcds;
-    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
     a.out_vec = a.out_row % (a.out_bf16 ? 8 : 4) == 0 && ((uintptr_t)a.out & 15) == 0;
     // rows of A within 32 bits of the first that a block reaches: its own always (K <= 2^22), any token's not always
     const bool wide = MODE == kHidden && a.T * a.a_row >= (int64_t)1 << 32;
@@ -782,7 +781,6 @@ template <bool HIDDEN> hipError_t launch_direct(const Args& a, int64_t items, hi
     const int64_t width = HIDDEN ? a.out_row : a.N;
     const auto blocks = [&](int nt) { return (width + 16 * nt - 1) / (16 * nt) * items; };
     const int nt = blocks(4) >= device_info().cus ? 4 : blocks(2) >= device_info().cus ? 2 : 1;
-    if (blocks(nt) >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
     note_launch("mx4_direct_kernel<%s,%d>", HIDDEN ? "hidden" : "output", nt);
     const dim3 grid((unsigned)blocks(nt));
     if (nt == 4) mx4_direct_kernel<HIDDEN, 4><<<grid, 64 * kTokenWaves, 0, s>>>(a);
@@ -1015,7 +1013,6 @@ __global__ __launch_bounds__(256) void clear_kernel(const int32_t* __restrict__ 
 
 template <bool A4, int MODE> hipError_t launch_rows(const Args& a, int64_t tiles, int mt, hipStream_t s) {
     const int64_t blocks = (a.N + 15) / 16 * tiles;
-    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
     note_launch("mx4_rows_kernel<%s,%d,%s>", A4 ? "mx4" : "bf16", mt,
                 MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : "output");
     const dim3 grid((unsigned)blocks);
@@ -1041,6 +1038,9 @@ int rows_tile(int64_t rows, int64_t N) {
     const auto fills = [&](int mt) { return (rows + 16 * mt - 1) / (16 * mt) * ((N + 15) / 16) >= kSmallEnoughBlocks; };
     return rows > 32 && fills(4) ? 4 : rows > 16 && fills(2) ? 2 : 1;
 }
+
+// whether a launch of mx4_rows_kernel, 512 threads a block, takes so many tiles of rows
+bool rows_fit(int64_t tiles, int64_t N) { return tiles * ((N + 15) / 16) < kMaxMx4Blocks / 2; }
 
 int64_t align256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -1087,12 +1087,12 @@ hipError_t launch_mx4_product(const Mx4Product& p, hipStream_t s) {
     a.act = p.act;
     a.out_bf16 = p.out_bf16;
     a.out_vec = p.N % 4 == 0 && ((uintptr_t)p.out & (p.out_bf16 ? 7 : 15)) == 0;
-    if (tiles_us(a4, (double)((p.T + 63) / 64), p.N, p.K) < rows_us(a4, (double)p.T, p.N, p.K)) {
+    const int mt = rows_tile(p.T, p.N);
+    if (tiles_us(a4, (double)((p.T + 63) / 64), p.N, p.K) < rows_us(a4, (double)p.T, p.N, p.K) || !rows_fit((p.T + 16 * mt - 1) / (16 * mt), p.N)) {
         const int tile_rows = tile_rows_for(p.T, p.N);
         const int64_t tiles = (p.T + tile_rows - 1) / tile_rows;
         return a4 ? launch_tiles<true, kDense>(a, tiles, tile_rows, s) : launch_tiles<false, kDense>(a, tiles, tile_rows, s);
     }
-    const int mt = rows_tile(p.T, p.N);
     const int64_t tiles = (p.T + 16 * mt - 1) / (16 * mt);
     return a4 ? launch_rows<true, kDense>(a, tiles, mt, s) : launch_rows<false, kDense>(a, tiles, mt, s);
 }
@@ -1151,7 +1151,8 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     const int64_t met = p.E < P ? p.E : P;
     const int mt = P / p.E <= 16 ? 1 : P / p.E <= 32 ? 2 : 4;
     const double rows = 16.0 * mt * (double)(P / (16 * mt) + met), rows64 = (double)(P / 64 + met);
-    const bool large = tiles_us(false, rows64, p.L, p.D) + tiles_us(false, rows64, p.O, p.L) < rows_us(false, rows, p.L, p.D) + rows_us(false, rows, p.O, p.L);
+    const bool large = tiles_us(false, rows64, p.L, p.D) + tiles_us(false, rows64, p.O, p.L) < rows_us(false, rows, p.L, p.D) + rows_us(false, rows, p.O, p.L) ||
+                       !rows_fit(P / (16 * mt) + met, p.L > p.O ? p.L : p.O);
     const int tile_rows = large ? tile_rows_for(P, p.L < p.O ? p.L : p.O) : 16 * mt;
     const int64_t tiles = P / tile_rows + met;
     int32_t *const count = words(at.count), *const start = words(at.start), *const tile_start = words(at.tile_start);
@@ -1200,12 +1201,18 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
         return hipGetLastError();
     }
     const int v = p.O % 8 == 0 && ((uintptr_t)p.out & 15) == 0 ? 8 : 1;
-    const int64_t blocks = (p.T * (p.O / v) + 255) / 256;
-    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
     note_launch("combine_kernel<%d>", v);
-    if (v == 8) combine_kernel<8><<<dim3((unsigned)blocks), 256, 0, s>>>(p.idx, p.weight, y, p.out, p.T, p.O, p.E, p.k);
-    else combine_kernel<1><<<dim3((unsigned)blocks), 256, 0, s>>>(p.idx, p.weight, y, p.out, p.T, p.O, p.E, p.k);
-    return hipGetLastError();
+    const int64_t most = ((kMaxMx4Blocks - 1) * 256) / (p.O / v);       // tokens of a launch
+    for (int64_t t = 0; t < p.T; t += most) {
+        const int64_t n = p.T - t < most ? p.T - t : most;
+        const dim3 grid((unsigned)((n * (p.O / v) + 255) / 256));
+        const int32_t* const idx = p.idx + t * p.k;
+        const float *const weight = p.weight ? p.weight + t * p.k : nullptr, *const from = y + t * p.k * p.O;
+        if (v == 8) combine_kernel<8><<<grid, 256, 0, s>>>(idx, weight, from, p.out + t * p.O, n, p.O, p.E, p.k);
+        else combine_kernel<1><<<grid, 256, 0, s>>>(idx, weight, from, p.out + t * p.O, n, p.O, p.E, p.k);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace fff

@@ -314,6 +314,27 @@ def test_leaves_few_tokens_of_many_wide_leaves(E, T):
     _within(out, want, 2 * k * 2.0 ** -24 * size + R.HALF["bf16"] * (np.abs(want) + 2 * k * 2.0 ** -24 * size), "biases")
 
 
+def test_leaves_with_more_results_than_a_launch_has_threads():
+    """Rows of an odd number of columns are mixed a column a thread, here in two launches.  Matrices of zeros: mixtures of the last biases."""
+    import torch
+    import paper_2308_14711_amd as F
+    T, D, L, O, k = (1 << 20) + 24, 32, 16, 4099, 2
+    z = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda")
+    b2 = torch.randn((2, O), device="cuda").bfloat16()
+    idx = torch.randint(0, 2, (T, k), device="cuda", dtype=torch.int32)
+    weight = torch.rand((T, k), device="cuda")
+    out = torch.full((T, O), -7.0, dtype=torch.bfloat16, device="cuda")
+    F.fff_leaf_forward_mx4(torch.zeros((T, D), dtype=torch.bfloat16, device="cuda"), z(2, L, 16), z(2, L, 1), torch.zeros((2, L), dtype=torch.bfloat16, device="cuda"),
+                           z(2, O, 16), z(2, O, 1), b2, idx, weight, F.ACT_RELU, out)
+    split = (((1 << 24) - 1) * 256) // O
+    assert split < T
+    for rows in (slice(0, 30), slice(split - 30, split + 30), slice(T - 30, T)):
+        parts = weight[rows].double()[:, :, None] * b2.double()[idx[rows].long()]
+        want, size = parts.sum(1).cpu().numpy(), parts.abs().sum(1).cpu().numpy()
+        # k products and sums in single precision, half a step of bf16
+        _within(out[rows], want, 2 * k * 2.0 ** -24 * size + R.HALF["bf16"] * (np.abs(want) + 2 * k * 2.0 ** -24 * size), "mixtures")
+
+
 def test_leaves_all_tokens_in_one_of_many():
     import torch
     import paper_2308_14711_amd as F
