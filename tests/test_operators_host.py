@@ -132,7 +132,7 @@ def test_refusals_of_sizes_that_no_launch_takes(L):
     assert q(0, 1, 1, (1 << 34) + 1) == SHAPE
     assert L.fff_mx4_dequantize(P(BIG), P(2 * BIG), P(3 * BIG), None, 1, (1 << 34) + 1, BF16) == SHAPE
     m = lambda T, N: L.fff_mx4_product(P(BIG), None, P(2 * BIG), P(3 * BIG), None, 2, P(4 * BIG), None, T, 32, N, BF16, None, 0)
-    assert m((1 << 31) - 1, 1) == RANGE and m(1 << 30, 129) == SHAPE           # (2^30 tokens are the most of any call)
+    assert m((1 << 31) - 1, 1) == RANGE and m(1 << 30, 129) == SHAPE           # (2^31 - 1024 tokens are the most of any call)
     assert L.fff_leaf_mx4_scratch_bytes(1 << 30, 32, 32, 4, 1, 16) == 0 and L.fff_leaf_mx4_scratch_bytes(1 << 20, 32, 129, 4, 16, 2000) > 0
     assert L.fff_leaf_mx4_scratch_bytes(1 << 26, 32, 32, 4, 8, 4097) == 0
 
