@@ -175,7 +175,11 @@ __device__ __forceinline__ float gelu_bulk(float v) {
     const float e = __builtin_amdgcn_rcpf(p);
     return 0.5f * v * (v >= 0.0f ? 2.0f - e : e);
 }
-__device__ __forceinline__ float apply(float v, int act, bool bf16) { return act == 2 ? v : act == 1 && bf16 ? gelu_bulk(v) : activate(v, act); }
+// (ReLU by a comparison: a maximum with 0 would turn NaN, which a block of scale 255 stands for, into 0)
+__device__ __forceinline__ float apply(float v, int act, bool bf16) {
+    if (act == 0) return v < 0.0f ? 0.0f : v;
+    return act == 2 ? v : bf16 ? gelu_bulk(v) : activate(v, act);
+}
 
 // sixteen bytes at any address
 __device__ __forceinline__ uint4 load_bytes(const uint8_t* p) {

@@ -1,0 +1,75 @@
+"""Values of the operators on four-bit matrices and routed experts where a launch could read them otherwise than the definition: NaN and
+infinity through activations, the tails of GELU, the roundings on the way, every scale byte, many tokens of few leaves."""
+import math
+
+import numpy as np
+import pytest
+
+import operators_reference as R
+from test_gpu_operators import _bytes, _leaf_case, _matrix, _up, _within
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- NaN and infinity through the activations ---------------------------------------------------------------
+
+# blocks of 16, 32 and 64 rows, then 64 and 128 rows through LDS
+PRODUCTS = [(5, 100, 40), (31, 100, 3100), (64, 100, 3100), (700, 1024, 1100), (3000, 264, 3200)]
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("kind", ["bf16", "mx4", "mx4-f32"])
+@pytest.mark.parametrize("size", PRODUCTS, ids=lambda s: "x".join(map(str, s)))
+def test_product_hands_on_nan_and_infinity(size, kind, act):
+    import torch
+    import paper_2308_14711_amd as F
+    T, K, N = size
+    rng = np.random.default_rng(T)
+    x = rng.normal(size=(T, K))
+    x[1, K - 1], x[3, 0] = np.nan, np.inf
+    rows, a = _up(x, "bf16")
+    wc, ws, _ = _matrix(rng, (N, K), 1.0)
+    ws[7, -1] = 255
+    w, kw, out_kind = R.values(wc, ws, K), {}, "f32" if kind == "mx4-f32" else "bf16"
+    if kind != "bf16":
+        ac, asc = R.quantise(a)
+        rows, kw, a = _bytes(ac), {"a_scales": _bytes(asc)}, R.values(ac, asc, K)
+    out = torch.empty((T, N), dtype=torch.float32 if out_kind == "f32" else torch.bfloat16, device="cuda")
+    F.fff_mx4_product(rows, _bytes(wc), _bytes(ws), out, act={"none": F.ACT_NONE, "relu": F.ACT_RELU, "gelu": F.ACT_GELU}[act], **kw)
+    some = np.unique(np.r_[0:5, T // 2, T - 2:T])
+    with np.errstate(invalid="ignore"):
+        want, tol = R.product(a[some], w, None, act, out_kind)
+    assert np.isnan(want[:, 7]).all() and np.isnan(want[1]).all() and np.isfinite(np.delete(want[[0, 2, 4]], 7, 1)).all()
+    _within(out[some.tolist()], want, tol, "product %s %s %s [%s]" % (size, kind, act, F.fff_last_launch()))
+
+
+# a block a token; few pairs of wide leaves; tiles of 16, 32 and 64 rows; of 64 and 128 through LDS
+LEAVES = [(20, 1, 8, 64, 40, 32), (5, 2, 4, 1096, 521, 601), (60, 1, 4, 520, 1024, 700), (40, 2, 3, 96, 40, 36), (150, 1, 3, 160, 130, 257),
+          (700, 2, 5, 296, 136, 300), (4100, 8, 2, 136, 1032, 1100)]
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("case", LEAVES, ids=lambda c: "-".join(map(str, c)))
+def test_leaves_hand_on_nan_and_infinity(case, act):
+    import torch
+    import paper_2308_14711_amd as F
+    T, k, E, D, O, width = case
+    rng = np.random.default_rng(T + width)
+    dev, (x, w1, b1, w2, b2, idx, weight) = _leaf_case(rng, *case, True, none=0.0)
+    dev = list(dev)
+    x[2, D - 1], x[1, 0] = np.nan, np.inf
+    dev[0] = _up(x, "bf16")[0]
+    # a block of a neuron of leaf 1, a block of an output of leaf 0; token 0 meets neither
+    c1, s1, c2, s2 = (dev[i].cpu().numpy() for i in (1, 2, 4, 5))
+    s1[1, 3, -1] = s2[0, 4, 0] = 255
+    w1, w2 = R.values(c1, s1, D), R.values(c2, s2, width)
+    idx[0] = E - 1 if E > 2 else -1
+    idx[3] = 1
+    dev[2], dev[5], dev[7] = _bytes(s1), _bytes(s2), _bytes(idx)
+    out = torch.full((T, O), -7.0, dtype=torch.bfloat16, device="cuda")
+    F.fff_leaf_forward_mx4(*dev, {"relu": F.ACT_RELU, "gelu": F.ACT_GELU}[act], out)
+    some = np.unique(np.r_[0:min(T, 20), T // 2, T - 2:T])
+    with np.errstate(invalid="ignore"):
+        want, tol = R.leaves(x[some], w1, b1, w2, b2, idx[some], weight[some], act)
+    assert np.isnan(want[2]).all() and np.isnan(want[3]).all() and np.isfinite(want[0]).all()
+    _within(out[some.tolist()], want, tol, "leaves %s %s" % (case, act))
