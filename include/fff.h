@@ -278,6 +278,8 @@ int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, v
  *   bias      [N] of `dtype`, or NULL
  *   act       FFF_ACT_NONE, FFF_ACT_RELU or FFF_ACT_GELU; of NaN all three are NaN, here and in fff_leaf_forward_mx4 (ReLU
  *             of NaN is 0 in the entry points without four-bit matrices)
+ *             GELU v Phi(v) before its rounding to bf16 (leaves' hidden activations too): within 2^-15 of its value for v >= -7, 2^-12 to
+ *             -11, 2^-10 below; in fp32 within (3 v^2 + 32) 2^-24 of it
  *   out       [T, N] of `dtype` (FFF_F32 only with a_scales: bf16 rows give bf16 results, else FFF_ERR_UNSUPPORTED)
  *   scratch   device memory, 256-byte aligned, of one call until its launches have run, at least
  *             fff_mx4_product_scratch_bytes: a copy of bf16 rows that are not whole aligned pieces of 16 bytes (K not a

@@ -73,3 +73,65 @@ def test_leaves_hand_on_nan_and_infinity(case, act):
         want, tol = R.leaves(x[some], w1, b1, w2, b2, idx[some], weight[some], act)
     assert np.isnan(want[2]).all() and np.isnan(want[3]).all() and np.isfinite(want[0]).all()
     _within(out[some.tolist()], want, tol, "leaves %s %s" % (case, act))
+
+
+# ---- GELU over its whole range -------------------------------------------------------------------------------
+
+# every bf16 value from 2^-10 to 8, and from -2^-10 to -13
+GRID = np.array([s * 2.0 ** e * (1 + m / 128) for s in (1, -1) for e in range(-10, 4) for m in range(128)])
+GRID = GRID[(GRID <= 8) & (GRID >= -13)]
+
+
+def _gelu(v):
+    return np.array([0.5 * x * math.erfc(-x / math.sqrt(2)) for x in v.ravel()]).reshape(v.shape)
+
+
+def _gelu_tol(v, kind):
+    """bf16: the kernels' own, relative to the value (2^-15 above -7, 2^-12 above -11, 2^-10 below), and half a step of the type.  fp32: the argument of
+    erfc rounded twice, which its square in the exponent carries 2 v^2 / 2 times on, and a few steps.  Values below the normal numbers may be zeros."""
+    y = np.abs(_gelu(v))
+    if kind == "f32":
+        return (3 * v * v + 32) * 2.0 ** -24 * y + 2.0 ** -122
+    own = np.where(v >= -7, 2.0 ** -15, np.where(v >= -11, 2.0 ** -12, 2.0 ** -10))
+    return y * (own + R.HALF["bf16"] * (1 + own)) + 2.0 ** -122
+
+
+@pytest.mark.parametrize("kind", ["bf16", "mx4", "mx4-f32"])
+@pytest.mark.parametrize("T", [3, 4096])
+def test_gelu_of_products(T, kind):
+    """Rows of zeros and a bias: the activation of the bias, through the small and the large launches."""
+    import torch
+    import paper_2308_14711_amd as F
+    out_kind = "f32" if kind == "mx4-f32" else "bf16"
+    v = GRID if out_kind == "bf16" else np.random.default_rng(0).uniform(-13, 8, size=4096).astype(np.float32).astype(np.float64)
+    N, u8 = len(v), torch.uint8
+    bias, back = _up(v, out_kind)
+    assert np.array_equal(back, v)
+    a, kw = torch.zeros((T, 32), dtype=torch.bfloat16, device="cuda"), {}
+    if kind != "bf16":
+        a, kw = torch.zeros((T, 16), dtype=u8, device="cuda"), {"a_scales": torch.full((T, 1), 127, dtype=u8, device="cuda")}
+    out = torch.empty((T, N), dtype=bias.dtype, device="cuda")
+    F.fff_mx4_product(a, torch.zeros((N, 16), dtype=u8, device="cuda"), torch.full((N, 1), 127, dtype=u8, device="cuda"), out, bias=bias, act=F.ACT_GELU, **kw)
+    assert (out == out[:1]).all()
+    _within(out[0], _gelu(v), _gelu_tol(v, out_kind), "gelu [%s]" % F.fff_last_launch())
+
+
+# a block a token; few pairs of wide leaves; tiles of rows; tiles through LDS
+@pytest.mark.parametrize("T,D", [(28, 32), (28, 4096), (224, 32), (11200, 1024)])
+def test_gelu_of_hidden_activations(T, D):
+    """Tokens of zeros, a hidden bias, and a last matrix of ones on the diagonal: each leaf's activations are its outputs."""
+    import torch
+    import paper_2308_14711_amd as F
+    E, L, u8 = 28, 128, torch.uint8
+    v = np.resize(GRID, E * L).reshape(E, L)
+    b1, _ = _up(v, "bf16")
+    c2, s2 = R.quantise(np.broadcast_to(np.eye(L), (E, L, L)))
+    idx = np.arange(T, dtype=np.int32) % E
+    out = torch.empty((T, L), dtype=torch.bfloat16, device="cuda")
+    nb = R.blocks(D)
+    F.fff_leaf_forward_mx4(torch.zeros((T, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((E, L, 16 * nb), dtype=u8, device="cuda"),
+                           torch.full((E, L, nb), 127, dtype=u8, device="cuda"), b1, _bytes(c2), _bytes(s2), torch.zeros((E, L), dtype=torch.bfloat16, device="cuda"),
+                           _bytes(idx), None, F.ACT_GELU, out)
+    assert (out.view(-1, E, L) == out[:E]).all()
+    # (a rounded activation times one, plus zeros)
+    _within(out[:E], _gelu(v), _gelu_tol(v, "bf16"), "gelu of %d tokens" % T)
