@@ -605,6 +605,10 @@ template <bool A4, int MODE> hipError_t launch_tiles(const Args& a, int64_t row_
     return tile_rows == 128 ? launch_tiles<A4, MODE, 8>(a, row_tiles, s) : launch_tiles<A4, MODE, 4>(a, row_tiles, s);
 }
 
+// Leaf networks, in every launch: a hidden activation is rounded to one bf16 value, the operand of the second product (a second value for what the first leaves would
+// double that product's matrix instructions: of 8192 tokens through 2 of 16 leaves, 768 - 2048 - 768, 71 of 168 us).  Everything after it is fp32: the
+// leaf's sums, its bias, the mixture weights, the sum over a token's leaves.
+
 // ---- a block a token ---------------------------------------------------------------------------------------
 //
 // Narrow leaves: one launch, no scratch.  All hidden activations of the token's k leaves (a wave's share of D, four tiles of 16 neurons at a
@@ -657,7 +661,6 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
     for (int i = 0; i < a.k; ++i) {
         const uint32_t e = (uint32_t)a.idx[t * a.k + i];
         if (e >= a.E) continue;                            // (not read below)
-        const float scale = a.weight ? a.weight[t * a.k + i] : 1.0f;
         for (int t0 = 0; t0 < h_tiles; t0 += kTokenTiles, round ^= 1) {
             const uint8_t *w_row[kTokenTiles], *ws_row[kTokenTiles];
             f32x4_t acc[kTokenTiles];
@@ -679,7 +682,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
                 float v = part[round][0][tid];
 #pragma unroll
                 for (int w = 1; w < kTokenWaves; ++w) v += part[round][w][tid];
-                v = n < a.N ? apply(v + bf16_to_f32(((const uint16_t*)a.bias)[(int64_t)e * a.N + n]), a.act, true) * scale : 0.f;
+                v = n < a.N ? apply(v + bf16_to_f32(((const uint16_t*)a.bias)[(int64_t)e * a.N + n]), a.act, true) : 0.f;
                 h[i * h_row + n] = f32_to_bf16(v);
             }
         }
@@ -688,24 +691,21 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
     const int64_t o_tiles = (b.N + 15) / 16;
     for (int64_t t0 = (int64_t)wv * kTokenTiles; t0 < o_tiles; t0 += kTokenWaves * kTokenTiles) {
         const int tiles = o_tiles - t0 < kTokenTiles ? (int)(o_tiles - t0) : kTokenTiles;
-        f32x4_t acc[kTokenTiles];
-        float bias[kTokenTiles][4];
+        f32x4_t sum[kTokenTiles];
 #pragma unroll
-        for (int u = 0; u < kTokenTiles; ++u) {
-            acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) bias[u][q] = 0.f;
-        }
+        for (int u = 0; u < kTokenTiles; ++u) sum[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         for (int i = 0; i < b.k; ++i) {
             const uint32_t e = (uint32_t)b.idx[t * b.k + i];
             if (e >= b.E) continue;
             const float scale = b.weight ? b.weight[t * b.k + i] : 1.0f;
             const uint8_t *w_row[kTokenTiles], *ws_row[kTokenTiles];
+            f32x4_t acc[kTokenTiles];
 #pragma unroll
             for (int u = 0; u < kTokenTiles; ++u) {
                 const int64_t n = 16 * (t0 + u) + j, r = (int64_t)e * b.N + (n < b.N ? n : b.N - 1);
                 w_row[u] = b.w + r * b.Kb * 16;
                 ws_row[u] = b.w_scales + r * b.Kb;
+                acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
             tiles_steps<kTokenTiles>(w_row, ws_row, tiles, (const char*)(h + i * h_row), b.Kb, b.pieces, g, 0, 1, acc);
             if (j == 0) {
@@ -714,16 +714,14 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int64_t n = 16 * (t0 + u) + 4 * g + q;
-                        if (n < b.N) bias[u][q] = fmaf(scale, bf16_to_f32(((const uint16_t*)b.bias)[(int64_t)e * b.N + n]), bias[u][q]);
+                        if (n < b.N) sum[u][q] = fmaf(scale, acc[u][q] + bf16_to_f32(((const uint16_t*)b.bias)[(int64_t)e * b.N + n]), sum[u][q]);
                     }
             }
         }
         if (j == 0) {
 #pragma unroll
             for (int u = 0; u < kTokenTiles; ++u) {
-                float o[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) o[q] = acc[u][q] + bias[u][q];
+                const float o[4] = {sum[u][0], sum[u][1], sum[u][2], sum[u][3]};
                 store4(b.out, true, b.out_vec, t * b.out_row, 16 * (t0 + u) + 4 * g, b.N, o);
             }
         }
@@ -732,8 +730,8 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
 
 // ---- few pairs of wide leaves ------------------------------------------------------------------------------
 //
-// Nothing to group: a block takes 16 NT columns of one pair's hidden activations (HIDDEN; h [pair], times the pair's weight) or of one token's
-// outputs (the sum over its pairs as one product along k rows of h and of W), K shared out among its waves.  Bound by the bytes of the weights.
+// Nothing to group: a block takes 16 NT columns of one pair's hidden activations (HIDDEN; h [pair]) or of one token's
+// outputs (its pairs one after another, each wave's part times the pair's weight), K shared out among its waves.  Bound by the bytes of the weights.
 template <bool HIDDEN, int NT>
 __global__ __launch_bounds__(64 * kTokenWaves, 4) void mx4_direct_kernel(const Args a) {
     __shared__ float part[kTokenWaves][16 * NT];
@@ -743,27 +741,34 @@ __global__ __launch_bounds__(64 * kTokenWaves, 4) void mx4_direct_kernel(const A
     const int k = HIDDEN ? 1 : a.k, steps = (a.Kb + 3) / 4;
     if (HIDDEN && (uint32_t)a.idx[item] >= a.E) return;            // (nobody reads its row)
     const int tiles = width - n0 < 16 * NT ? (int)((width - n0 + 15) / 16) : NT;
-    f32x4_t acc[NT];
+    f32x4_t sum[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) sum[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < k; ++i) {
         const int64_t pair = item * k + i;
         const uint32_t e = (uint32_t)a.idx[pair];
         if (e >= a.E) continue;
         const uint8_t *w_row[NT], *ws_row[NT];
+        f32x4_t acc[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int64_t n = n0 + 16 * t + j, r = (int64_t)e * a.N + (n < a.N ? n : a.N - 1);
             w_row[t] = a.w + r * a.Kb * 16;
             ws_row[t] = a.w_scales + r * a.Kb;
+            acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
         // (step c of pair i is step i * steps + c of the sum: waves that pair i leaves without a step begin with pair i + 1)
         tiles_steps<NT>(w_row, ws_row, tiles, a.a + (HIDDEN ? pair / a.k : pair) * a.a_row, a.Kb, a.pieces, g,
                         (wv + kTokenWaves - i * steps % kTokenWaves) % kTokenWaves, kTokenWaves, acc);
+        const float scale = !HIDDEN && a.weight ? a.weight[pair] : 1.0f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[t][q] = fmaf(scale, acc[t][q], sum[t][q]);
     }
     if (j == 0) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) *(f32x4_t*)&part[wv][16 * t + 4 * g] = acc[t];
+        for (int t = 0; t < NT; ++t) *(f32x4_t*)&part[wv][16 * t + 4 * g] = sum[t];
     }
     __syncthreads();
     const int64_t n = n0 + tid;
@@ -776,7 +781,7 @@ __global__ __launch_bounds__(64 * kTokenWaves, 4) void mx4_direct_kernel(const A
         const uint32_t e = (uint32_t)a.idx[pair];
         if (e >= a.E || n >= a.N) continue;
         const float scale = a.weight ? a.weight[pair] : 1.0f, bias = bf16_to_f32(((const uint16_t*)a.bias)[(int64_t)e * a.N + n]);
-        v = HIDDEN ? apply(v + bias, a.act, true) * scale : fmaf(scale, bias, v);
+        v = HIDDEN ? apply(v + bias, a.act, true) : fmaf(scale, bias, v);
     }
     if (HIDDEN && n >= a.N) v = 0.f;
     ((uint16_t*)a.out)[item * a.out_row + n] = f32_to_bf16(v);

@@ -135,3 +135,32 @@ def test_gelu_of_hidden_activations(T, D):
     assert (out.view(-1, E, L) == out[:E]).all()
     # (a rounded activation times one, plus zeros)
     _within(out[:E], _gelu(v), _gelu_tol(v, "bf16"), "gelu of %d tokens" % T)
+
+
+# ---- where the leaves' values are rounded ----------------------------------------------------------------------
+
+
+# a block a token; few pairs of wide leaves; tiles of rows; tiles through LDS
+@pytest.mark.parametrize("T,D,k", [(20, 32, 1), (6, 32, 4), (20, 4096, 1), (7, 4096, 3), (300, 32, 2), (6000, 1024, 2)])
+def test_mixture_weights_meet_sums_not_activations(T, D, k):
+    """Hidden activations that bf16 holds exactly, pairs of which almost cancel: a weight that met them before their rounding would leave an
+    error of their size, not of the difference's."""
+    import torch
+    import paper_2308_14711_amd as F
+    E, L, O, u8 = 6, 128, 64, torch.uint8
+    rng = np.random.default_rng(T + k)
+    h = rng.integers(128, 256, size=(E, L)) / 128.0                       # 1 to 2 in steps of 2^-7
+    w2 = np.zeros((E, O, L))
+    w2[:, np.arange(O), np.arange(O)], w2[:, np.arange(O), np.arange(O) + O] = 1, -1
+    c2, s2 = R.quantise(w2)
+    idx = rng.integers(0, E, size=(T, k)).astype(np.int32)
+    weight = rng.normal(size=(T, k)).astype(np.float32)
+    out, nb = torch.empty((T, O), dtype=torch.bfloat16, device="cuda"), R.blocks(D)
+    F.fff_leaf_forward_mx4(torch.zeros((T, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((E, L, 16 * nb), dtype=u8, device="cuda"),
+                           torch.full((E, L, nb), 127, dtype=u8, device="cuda"), _up(h, "bf16")[0], _bytes(c2), _bytes(s2),
+                           torch.zeros((E, O), dtype=torch.bfloat16, device="cuda"), _bytes(idx), _bytes(weight), F.ACT_RELU, out)
+    parts = weight.astype(np.float64)[:, :, None] * (h[:, :O] - h[:, O:])[idx]
+    want, size = parts.sum(1), np.abs(parts).sum(1)
+    # the differences are exact; k products and sums in single precision, half a step of bf16
+    tol = 2 * k * 2.0 ** -24 * size
+    _within(out, want, tol + R.HALF["bf16"] * (np.abs(want) + tol), "mixture of %d tokens" % T)
