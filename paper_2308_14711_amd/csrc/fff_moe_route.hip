@@ -134,8 +134,16 @@ template <bool BF16, int V, bool VEC> struct RawRow {
     }
 };
 
-// exp(l - m) for l <= m, m finite.  (The product with log2(e) is rounded once more: a relative 2^-24 |l - m|, as much as the difference's.)
-__device__ __forceinline__ float relative(float l, float m) { return __builtin_amdgcn_exp2f((l - m) * 1.44269504f); }
+// exp(l - m) for l <= m, m finite.  With y the rounded product of x = l - m and log2(e), exp(x) = 2^y exp(x - y ln 2), and x - y ln 2, ln 2 in two parts, is what the
+// product's rounding left: without it the error grows with m - l, 2^-24 (m - l) and more, as much again as the difference's own (32768 x 512 fp32 logits,
+// k = 8, and the gradient: 67.7 us without, 69.3 with).
+__device__ __forceinline__ float relative(float l, float m) {
+    const float x = fmaxf(l - m, -200.0f);       // (exp(-200) is 0 in fp32)
+    const float y = x * 1.44269504f;
+    const float rest = fmaf(y, 1.904654e-9f, fmaf(y, -0.693147182f, x));
+    const float r = __builtin_amdgcn_exp2f(y);
+    return fmaf(r, rest, r);
+}
 // The same for any m: logits of +infinity share the row.
 __device__ __forceinline__ float share_of(float l, float m) { return m == __builtin_inff() ? (l == m ? 1.0f : 0.0f) : relative(l, m); }
 // All of a row's (zeros where it has none).

@@ -164,3 +164,36 @@ def test_mixture_weights_meet_sums_not_activations(T, D, k):
     # the differences are exact; k products and sums in single precision, half a step of bf16
     tol = 2 * k * 2.0 ** -24 * size
     _within(out, want, tol + R.HALF["bf16"] * (np.abs(want) + tol), "mixture of %d tokens" % T)
+
+
+# ---- routing: shares far below the largest ---------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("E", [2, 60, 130, 600, 1500])
+def test_shares_far_below_the_largest(E, normalise):
+    """Differences of logits that single precision holds exactly: only the exponential is rounded, whose error does not grow with the difference."""
+    import torch
+    import paper_2308_14711_amd as F
+    gap = np.arange(1, 641) / 8.0                                  # up to 80
+    T = len(gap)
+    l = np.full((T, E), -np.inf)
+    l[:, E // 2] = 3.0
+    l[:, E - 1 if E > 2 else 0] = 3.0 - gap
+    logits, lv = _up(l)
+    assert np.array_equal(lv, l)
+    idx, w = torch.empty((T, 2), dtype=torch.int32, device="cuda"), torch.empty((T, 2), device="cuda")
+    count = torch.empty((E + 1,), dtype=torch.int32, device="cuda")
+    F.fff_moe_route(logits, 2, idx, w, count, normalise=normalise)
+    want = R.route(l, 2, None, normalise)
+    assert np.array_equal(idx.cpu().numpy(), want[0])
+    # the exponential (two steps of 2^-23, and the product before it carried in two parts: one), a sum and a division
+    few = 8 * 2.0 ** -24
+    _within(w, want[1], few * want[1], "weights")
+    # the gradient of the smaller weight: w0 w1 at both, through as many roundings again
+    dw = np.zeros((T, 2), np.float32)
+    dw[:, 1] = 1
+    d = torch.empty((T, E), device="cuda")
+    F.fff_moe_route_backward(logits, idx, count, d, dweight=_bytes(dw), normalise=normalise)
+    g, size = R.route_backward(l, want[0], want[2], dw, None, None, normalise)
+    _within(d, g, 3 * few * size, "dlogits")
