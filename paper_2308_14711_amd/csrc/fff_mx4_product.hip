@@ -914,7 +914,9 @@ __global__ __launch_bounds__(256) void group_place_kernel(const int32_t* __restr
 }
 
 // Two launches while all blocks' counts are few: each block's own, then every block adds up those before it, scans the leaves and places its pairs.
-constexpr int64_t kGroupWords = 8192, kGroupTwoLeaves = 4000;     // counts of all blocks; leaves whose four tables fit 64 KB of LDS
+// A leaf's counts are a thread's, so the work is quadratic in the blocks (pairs of 1, 4 and 16 leaves, whole forward, two launches / four: 65536 24.2 / 25.6 us,
+// 27.2 / 28.2, 28.4 / 29.9; 131072 37.1 / 37.9, 46.1 / 45.1, 47.2 / 46.9; 262144 71.8 / 70.5, 80.8 / 76.3, 80.0 / 76.7; of one leaf 8 million 5357 / 2733).
+constexpr int64_t kGroupWords = 8192, kGroupTwoLeaves = 4000, kGroupTwoBlocks = 128;     // counts of all blocks; leaves whose four tables fit 64 KB of LDS
 __global__ __launch_bounds__(1024) void group_hist_kernel(const int32_t* __restrict__ idx, int64_t P, int E, int32_t* __restrict__ counts) {
     extern __shared__ int32_t own[];
     for (int e = threadIdx.x; e < E; e += 1024) own[e] = 0;
@@ -1171,7 +1173,7 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     if (P <= kGroupOnePairs && p.E <= kGroupOneLeaves) {
         note_launch("group_one_kernel");
         group_one_kernel<<<1, 1024, (size_t)(3 * p.E + 2) * 4, s>>>(p.idx, (int)P, (int)p.E, tile_rows, start, tile_start, perm, tile_leaf, tile_slot);
-    } else if (p.E <= kGroupTwoLeaves && (P + kGroupPairs - 1) / kGroupPairs * p.E <= kGroupWords) {
+    } else if (p.E <= kGroupTwoLeaves && P <= kGroupTwoBlocks * kGroupPairs && (P + kGroupPairs - 1) / kGroupPairs * p.E <= kGroupWords) {
         const dim3 blocks((unsigned)((P + kGroupPairs - 1) / kGroupPairs));
         note_launch("group_hist_kernel");
         group_hist_kernel<<<blocks, 1024, (size_t)p.E * 4, s>>>(p.idx, P, (int)p.E, count);

@@ -197,3 +197,32 @@ def test_shares_far_below_the_largest(E, normalise):
     F.fff_moe_route_backward(logits, idx, count, d, dweight=_bytes(dw), normalise=normalise)
     g, size = R.route_backward(l, want[0], want[2], dw, None, None, normalise)
     _within(d, g, 3 * few * size, "dlogits")
+
+
+# ---- many tokens of few leaves ---------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("E,T,k", [(1, 5000, 1), (1, 131072, 1), (1, 131073, 1), (2, 50001, 2), (3, 200003, 1), (16, 65536, 2), (16, 65537, 2), (64, 131071, 1),
+                                   (130, 65000, 1), (125, 66000, 1)])
+def test_many_tokens_of_few_leaves(E, T, k):
+    """Matrices of zeros: a token is the mixture of its leaves' last biases, whichever launches group the pairs."""
+    import torch
+    import paper_2308_14711_amd as F
+    D, L, O = 32, 16, 16
+    z = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn((T, D), generator=g, device="cuda").bfloat16()
+    b2 = torch.randn((E, O), generator=g, device="cuda").bfloat16()
+    idx = torch.randint(-1, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    weight = torch.rand((T, k), generator=g, device="cuda")
+    out = torch.full((T, O), -7.0, dtype=torch.bfloat16, device="cuda")
+    F.fff_leaf_forward_mx4(x, z(E, L, 16), z(E, L, 1), torch.zeros((E, L), dtype=torch.bfloat16, device="cuda"), z(E, O, 16), z(E, O, 1), b2, idx, weight,
+                           F.ACT_RELU, out)
+    # 128 blocks of 1024 pairs are the most of which each adds up all counts (work that grows with their square), 8192 counts in all
+    two = T * k <= 1 << 17 and -(-T * k // 1024) * E <= 8192
+    assert ("group_spread_kernel" in F.fff_last_launch()) == two, F.fff_last_launch()
+    parts = weight.double()[:, :, None] * torch.where(idx[:, :, None] < 0, 0.0, b2.double()[idx.clamp_min(0).long()])
+    want, size = parts.sum(1).cpu().numpy(), parts.abs().sum(1).cpu().numpy()
+    # k products and sums in single precision, half a step of bf16
+    tol = 2 * k * 2.0 ** -24 * size
+    _within(out, want, tol + R.HALF["bf16"] * (np.abs(want) + tol), "biases")
