@@ -284,7 +284,7 @@ int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, v
  *   scratch   device memory, 256-byte aligned, of one call until its launches have run, at least
  *             fff_mx4_product_scratch_bytes: a copy of bf16 rows that are not whole aligned pieces of 16 bytes (K not a
  *             multiple of 8, or a misaligned); never read otherwise, and may be NULL then
- * K <= 2^22, N <= 2^22, fewer than 2^24 tiles of 128 x 128 results (else FFF_ERR_SHAPE).  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T), FFF_ERR_SHAPE, FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (act, or misaligned codes),
+ * K <= 2^22, N <= 2^22, at most 2^24 - 8 tiles of 128 x 128 results (else FFF_ERR_SHAPE).  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T), FFF_ERR_SHAPE, FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (act, or misaligned codes),
  * FFF_ERR_ALIAS (out or scratch overlaps an input or each other), FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.
  */
 int fff_mx4_product(const void* a, const uint8_t* a_scales, const uint8_t* w, const uint8_t* w_scales,
@@ -305,7 +305,7 @@ size_t fff_mx4_product_scratch_bytes(int64_t T, int64_t K);
  *   scratch  device memory, 256-byte aligned, of one call until its launches have run, at least
  *            fff_leaf_mx4_scratch_bytes of the same sizes; needs no initial value
  * Hidden activations are rounded to bf16 (the operand type of the matrix cores); sums, and their products with the weights, are fp32.  Results do not depend on the
- * order in which tokens are grouped.  D and O <= 2^22, and fewer than 2^24 tiles of 64 tokens x 128 columns (a part of one for every leaf;
+ * order in which tokens are grouped.  D and O <= 2^22, and at most 2^24 - 8 tiles of 64 tokens x 128 columns (a part of one for every leaf;
  * else FFF_ERR_SHAPE).  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T, k, n_leaves, leaf_width), FFF_ERR_SHAPE, FFF_ERR_DTYPE,
  * FFF_ERR_UNSUPPORTED, FFF_ERR_ALIAS, FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.
  */

@@ -1199,7 +1199,7 @@ int fff_mx4_product(const void* a, const uint8_t* a_scales, const uint8_t* w, co
     if (dtype != FFF_F32 && dtype != FFF_BF16) return FFF_ERR_DTYPE;
     if (T < 0 || T > kMaxTokens) return FFF_ERR_RANGE;
     if (K < 1 || N < 1 || K > kMaxMx4Side || N > kMaxMx4Side || T * mx_blocks(K) > (kMaxElems >> 5) || T * N > kMaxElems ||
-        N * mx_blocks(K) > (kMaxElems >> 5) || ((T + 127) / 128) * ((N + 127) / 128) >= kMaxMx4Blocks)
+        N * mx_blocks(K) > (kMaxElems >> 5) || ((T + 127) / 128) * ((N + 127) / 128) > kMaxMx4Tiles)
         return FFF_ERR_SHAPE;
     if (act != FFF_ACT_RELU && act != FFF_ACT_GELU && act != FFF_ACT_NONE) return FFF_ERR_UNSUPPORTED;
     if (!a_scales && dtype != FFF_BF16) return FFF_ERR_UNSUPPORTED;
@@ -1242,7 +1242,7 @@ static int check_leaf_mx4(int64_t T, int64_t D, int64_t O, int64_t n_leaves, int
     const int64_t m = (D > O ? D : O) + kMxBlock, l = leaf_width + kMxBlock;
     if (m > kMaxElems / rows || l > kMaxElems / rows || n_leaves * l > kMaxElems / m) return FFF_ERR_SHAPE;
     const int64_t met = T * k < n_leaves ? T * k : n_leaves, columns = O > leaf_width ? O : leaf_width;
-    if ((T * k / 64 + met) * ((columns + 127) / 128) >= kMaxMx4Blocks) return FFF_ERR_SHAPE;
+    if ((T * k / 64 + met) * ((columns + 127) / 128) > kMaxMx4Tiles) return FFF_ERR_SHAPE;
     return FFF_OK;
 }
 

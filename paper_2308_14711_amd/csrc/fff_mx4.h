@@ -9,6 +9,7 @@ constexpr int kMxBlock = 32;                       // elements that share a scal
 constexpr int64_t kMaxExperts = 4096;              // of launch_route
 constexpr int kMaxChoices = 32;                    // experts per token
 constexpr int64_t kMaxMx4Blocks = 1 << 24;         // a launch ends at 2^32 threads: fewer blocks of 256
+constexpr int64_t kMaxMx4Tiles = kMaxMx4Blocks - 8;  // of a product: as many blocks for each of the eight XCDs
 constexpr int64_t kMaxMx4Row = (int64_t)1 << 34;   // elements of a row to quantise or read back: its pieces are threads of a launch
 inline int64_t mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 
