@@ -1163,7 +1163,7 @@ int fff_mx4_quantize(const void* src, uint8_t* codes, uint8_t* scales, int trans
     if (batch == 0) return FFF_OK;
     // (blocks of 32 and tiles of columns count whole: 2^40 of either is the limit too)
     if (batch > kMaxElems / (rows * cols) || batch * (transpose ? cols : rows) > (kMaxElems >> 5) / mx_blocks(transpose ? rows : cols)) return FFF_ERR_SHAPE;
-    if (transpose ? batch >= kMaxMx4Blocks / (((rows + 127) / 128) * ((cols + 63) / 64)) : cols > kMaxMx4Row) return FFF_ERR_SHAPE;
+    if (transpose ? batch > (kMaxMx4Blocks - 1) / (((rows + 127) / 128) * ((cols + 63) / 64)) : cols > kMaxMx4Row) return FFF_ERR_SHAPE;
     if (!src || !codes || !scales) return FFF_ERR_NULL;
     if (!aligned16(codes)) return FFF_ERR_UNSUPPORTED;
     const int64_t blocks = batch * (transpose ? cols * mx_blocks(rows) : rows * mx_blocks(cols));

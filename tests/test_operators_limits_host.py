@@ -33,3 +33,12 @@ def test_tiles_of_a_product_are_a_whole_number_for_each_xcd(L):
     assert leaves(most)
     for tiles in range(most + 1, most + 9):
         assert not leaves(tiles), tiles
+
+
+def test_tiles_of_columns_to_quantise_end_at_a_launch(L):
+    """2^24 tiles of 128 rows x 64 columns are one too many, whatever the tiles of a matrix."""
+    def refused(batch, rows, cols):
+        return L.fff_mx4_quantize(None, P(2 * BIG), P(3 * BIG), 1, None, batch, rows, cols, BF16) == SHAPE
+    for rows, cols, tiles in ((1, 1, 1), (1, 129, 3), (300, 64, 3), (129, 200, 8), (640, 1, 5)):
+        batch = ((1 << 24) - 1) // tiles
+        assert not refused(batch, rows, cols) and refused(batch + 1, rows, cols), (rows, cols)
