@@ -183,13 +183,6 @@ __device__ __forceinline__ float apply(float v, int act, bool bf16) {
     return act == 2 ? v : bf16 ? gelu_bulk(v) : gelu_f32(v);
 }
 
-// sixteen bytes at any address
-__device__ __forceinline__ uint4 load_bytes(const uint8_t* p) {
-    typedef u32x4_t u32x4_byte_t __attribute__((aligned(1)));
-    const u32x4_t v = *(const u32x4_byte_t*)p;
-    return make_uint4(v.x, v.y, v.z, v.w);
-}
-
 // four consecutive outputs n .. n + 3 of a row, those below `limit`
 __device__ __forceinline__ void store4(char* out, bool bf16, bool vec, int64_t at, int64_t n, int64_t limit, const float* v) {
     if (bf16) {
