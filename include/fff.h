@@ -264,7 +264,8 @@ int fff_moe_route_backward(const void* logits, const uint8_t* token_mask, int64_
  * FFF_ERR_DTYPE, FFF_ERR_UNSUPPORTED (codes misaligned), FFF_ERR_ALIAS (codes or scales overlap src or each other), FFF_ERR_DEVICE.
  * batch == 0 is FFF_OK.
  *
- * fff_mx4_dequantize: the values, [rows, cols] of `dtype` (exact in both); the same errors, FFF_ERR_RANGE for rows < 0.
+ * fff_mx4_dequantize: the values, [rows, cols] of `dtype`: exact in both, but for those of 2^128 and more, which no quantisation makes (codes of 4 and 6
+ * at scale 253; of 2, 3, 4 and 6 at 254) and which are infinities; the same errors, FFF_ERR_RANGE for rows < 0.
  */
 int fff_mx4_quantize(const void* src, uint8_t* codes, uint8_t* scales, int transpose, void* stream,
                      int64_t batch, int64_t rows, int64_t cols, int dtype);
@@ -272,7 +273,8 @@ int fff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, void* out, v
                        int64_t cols, int dtype);
 
 /*
- * fff_mx4_product: out = act(A W^T + bias) with W in four bits; fp32 accumulation, one rounding at the end.
+ * fff_mx4_product: out = act(A W^T + bias) with W in four bits; fp32 accumulation, one rounding at the end.  bf16 rows meet W's values as bf16 has
+ * them (2^128 and more: infinities), rows of codes meet its scales and codes as they are.
  *   a         [T, K]: bf16 when a_scales is NULL, else codes with scales a_scales (fff_mx4_quantize)
  *   w, w_scales   codes and scales of [N, K]
  *   bias      [N] of `dtype`, or NULL
@@ -300,6 +302,7 @@ size_t fff_mx4_product_scratch_bytes(int64_t T, int64_t K);
  *   x [T, D] bf16; leaf_w1, leaf_s1: codes and scales of [n_leaves, leaf_width, D]; leaf_b1 [n_leaves, leaf_width];
  *   leaf_w2, leaf_s2: codes and scales of [n_leaves, O, leaf_width] (of leaf_w2 [n_leaves, leaf_width, O]:
  *   fff_mx4_quantize with transpose); leaf_b2 [n_leaves, O]; biases bf16
+ *   (the matrices' values as bf16 has them: fff_mx4_product)
  *   leaf_idx [T, k] int32, weight [T, k] fp32 or NULL (ones); k 1..32; n_leaves 1..65536; leaf_width 1..65536
  *   act FFF_ACT_RELU or FFF_ACT_GELU; out [T, O] bf16, must not overlap x; dtype must be FFF_BF16 (else FFF_ERR_UNSUPPORTED)
  *   scratch  device memory, 256-byte aligned, of one call until its launches have run, at least

@@ -4,7 +4,7 @@
 // (j = lane mod 16, g = lane / 16) takes block 4 c + g of row j in step c, 16 bytes of codes and one scale byte, so a step covers
 // 128 elements of K and every load is a whole block.  K is only an order of summation, so the rows of A are read the same way.
 //   A in bf16: the lane's 32 codes become four operands of v_mfma_f32_16x16x32_bf16 (eight elements of K per lane each): the
-//     conversion instruction multiplies by the scale, and code times scale is exact in bf16.
+//     conversion instruction multiplies by the scale, and code times scale is exact in bf16 (infinity from 2^128 on, which scales 253 and 254 reach).
 //   A in four bits: the 16 bytes are the operand of v_mfma_scale_f32_16x16x128_f8f6f4 as they are, with a scale byte per lane.
 // Rows of W are the rows of the result, rows of A its columns: lane (j, g) ends with four consecutive outputs of token j.
 #include "fff_device.h"

@@ -166,6 +166,57 @@ def test_mixture_weights_meet_sums_not_activations(T, D, k):
     _within(out, want, tol + R.HALF["bf16"] * (np.abs(want) + tol), "mixture of %d tokens" % T)
 
 
+# ---- every scale byte ------------------------------------------------------------------------------------------
+
+
+def _every_code():
+    """[256 scale bytes x 16 codes] rows of one block whose first element is the code, and the element's value."""
+    c, s = np.zeros((256, 16, 16), np.uint8), np.zeros((256, 16, 1), np.uint8)
+    c[:, :, 0], s[:, :, 0] = np.arange(16), np.arange(256)[:, None]
+    c, s = c.reshape(4096, 16), s.reshape(4096, 1)
+    return c, s, R.values(c, s, 1)[:, 0]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_values_of_every_scale_byte_and_code(kind):
+    """Values of 2^128 and more (4 and 6 at byte 253; 2, 3, 4 and 6 at 254) are infinities in either type; all others are exact, 255 is NaN."""
+    import torch
+    import paper_2308_14711_amd as F
+    c, s, v = _every_code()
+    for cols in (1, 8, 32):
+        out = torch.empty((4096, cols), dtype=torch.float32 if kind == "f32" else torch.bfloat16, device="cuda")
+        F.fff_mx4_dequantize(_bytes(c), _bytes(s), out)
+        want = np.where(np.abs(v) >= 2.0 ** 128, np.copysign(np.inf, v), v)
+        got = out.float().cpu().numpy().astype(np.float64)
+        assert np.array_equal(got[:, 0], want, equal_nan=True)
+        assert np.isnan(got[4080:]).all() and not got[:4080, 1:].any()
+
+
+@pytest.mark.parametrize("power", [-120, -60, 0, 60, 120])
+@pytest.mark.parametrize("kind", ["bf16", "mx4"])
+@pytest.mark.parametrize("T", [3, 4096])
+def test_products_of_every_scale_byte_and_code(T, kind, power):
+    """A power of two in every row against every code at every scale, through the small and the large launches.  bf16 rows meet the value as
+    bf16 holds it, infinities included; rows of codes meet scale and code as they are."""
+    import torch
+    import paper_2308_14711_amd as F
+    c, s, v = _every_code()
+    if kind == "bf16":
+        a, kw = torch.zeros((T, 32), dtype=torch.bfloat16, device="cuda"), {}
+        a[:, 0] = 2.0 ** power
+        v = np.where(np.abs(v) >= 2.0 ** 128, np.copysign(np.inf, v), v)
+    else:
+        a, kw = torch.zeros((T, 16), dtype=torch.uint8, device="cuda"), {"a_scales": torch.full((T, 1), 127 + power, dtype=torch.uint8, device="cuda")}
+        a[:, 0] = 2                                       # 1.0
+    out = torch.empty((T, 4096), dtype=torch.bfloat16, device="cuda")
+    F.fff_mx4_product(a, _bytes(c), _bytes(s), out, **kw)
+    assert torch.equal(out.view(torch.int16), out[:1].view(torch.int16).expand(T, -1))
+    want = v * 2.0 ** power
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+    # exact, but for results below the normal numbers, which may be zeros
+    _within(out[0], want, np.where(np.abs(want) < 2.0 ** -126, 2.0 ** -126, 0.0), "2^%d [%s]" % (power, F.fff_last_launch()))
+
+
 # ---- routing: shares far below the largest ---------------------------------------------------------------------
 
 
