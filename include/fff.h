@@ -222,9 +222,9 @@ int fff_moe_top1_forward(const void* x, const void* gate_w, const void* gate_b,
  *   scratch     device memory, 256-byte aligned, at least fff_route_scratch_bytes of the same sizes, of one
  *               call from its launches until they have run; needs no initial value.  Only read where one of
  *               count, prob_mean and loss is given (they are then written for T = 0 too); else it may be NULL.
- * Sums are fp32 in an order that depends on the sizes alone.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T,
- * n_experts, k), FFF_ERR_SHAPE (T * n_experts beyond 2^40), FFF_ERR_DTYPE, FFF_ERR_WORKSPACE, FFF_ERR_ALIAS (an output overlaps logits or
- * scratch), FFF_ERR_DEVICE.
+ * Sums are fp32 in an order that depends on the sizes, the type, the alignment of logits and the device alone.  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T,
+ * n_experts, k), FFF_ERR_SHAPE (T * n_experts beyond 2^40), FFF_ERR_DTYPE, FFF_ERR_WORKSPACE, FFF_ERR_ALIAS (an output or scratch
+ * overlaps an input or another output), FFF_ERR_DEVICE.
  */
 int fff_moe_route(const void* logits, const uint8_t* token_mask, int64_t n_experts, int k, int normalise,
                   int32_t* expert_idx, float* weight, int32_t* count, float* prob_mean, float* loss,

@@ -180,8 +180,8 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const uint16_t* __restric
     }
 }
 
-// Rows a pass over the grid takes (every one of its `pieces` places has a thread) and the blocks for them: about eight
-// passes' worth of threads a compute unit can hold, fewer for small matrices.
+// Rows a pass over the grid takes (every one of its `pieces` places has a thread) and the blocks for them: as many threads as the compute units
+// hold at once, fewer for small matrices.
 int64_t rows_a_pass(int64_t rows, int64_t pieces, int64_t* blocks) {
     const int64_t threads = (int64_t)device_info().cus * 2048;
     int64_t step = threads / pieces;
