@@ -307,7 +307,7 @@ size_t fff_mx4_product_scratch_bytes(int64_t T, int64_t K);
  *   act FFF_ACT_RELU or FFF_ACT_GELU; out [T, O] bf16, must not overlap x; dtype must be FFF_BF16 (else FFF_ERR_UNSUPPORTED)
  *   scratch  device memory, 256-byte aligned, of one call until its launches have run, at least
  *            fff_leaf_mx4_scratch_bytes of the same sizes; needs no initial value
- * Hidden activations are rounded to bf16 (the operand type of the matrix cores); sums, and their products with the weights, are fp32.  Results do not depend on the
+ * Hidden activations enter the second product as two bf16 values (within 2^-15 of them); sums, and their products with the weights, are fp32.  Results do not depend on the
  * order in which tokens are grouped.  D and O <= 2^22, and at most 2^24 - 8 tiles of 64 tokens x 128 columns (a part of one for every leaf;
  * else FFF_ERR_SHAPE).  Errors: FFF_ERR_NULL, FFF_ERR_RANGE (T, k, n_leaves, leaf_width), FFF_ERR_SHAPE, FFF_ERR_DTYPE,
  * FFF_ERR_UNSUPPORTED, FFF_ERR_ALIAS, FFF_ERR_WORKSPACE, FFF_ERR_DEVICE.

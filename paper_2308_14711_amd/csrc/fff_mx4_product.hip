@@ -42,7 +42,7 @@ struct Args {
     const void* bias;            // may be null
     char* out;
     int64_t T, N;                // rows of A, rows of W (of one leaf)
-    int64_t out_row;             // elements from row to row of out
+    int64_t out_row;             // elements from row to row of out (hidden activations: of each of a row's two values)
     int Kb, pieces;              // blocks of a row of W; whole pieces of 16 bytes of a bf16 row
     int act;
     bool out_bf16, out_vec;      // out_vec: four consecutive outputs are one aligned store
@@ -56,6 +56,7 @@ struct Args {
     const int32_t* n_tiles;
     int64_t E;
     int k;
+    int parts;                   // blocks that share a tile's rows (output launches)
 };
 
 __device__ __forceinline__ bf16x8_t dequantise8(uint32_t codes, float scale) {
@@ -72,12 +73,12 @@ __device__ __forceinline__ f32x4_t mfma4(const uint4& w, uint32_t ws, const uint
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, va, acc, 4, 4, BYTE, (int)ws, BYTE, (int)as);
 }
 
-// One step of 128 elements: a block of 32 of this lane's row of W against MT rows of A (A in bf16: four pieces each).
-template <bool A4, int MT>
-__device__ __forceinline__ void multiply128(const uint4& w, uint32_t ws, const uint4 (&a)[MT][A4 ? 1 : 4], const uint32_t (&as)[MT], f32x4_t (&acc)[MT]) {
+// One step of 128 elements: a block of 32 of this lane's row of W against VALUES rows of each of MT rows of A (A in bf16: four pieces each).
+template <bool A4, int MT, int VALUES>
+__device__ __forceinline__ void multiply128(const uint4& w, uint32_t ws, const uint4 (&a)[VALUES][MT][A4 ? 1 : 4], const uint32_t (&as)[MT], f32x4_t (&acc)[MT]) {
     if constexpr (A4) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) acc[m] = mfma4(w, ws, a[m][0], as[m], acc[m]);
+        for (int m = 0; m < MT; ++m) acc[m] = mfma4(w, ws, a[0][m][0], as[m], acc[m]);
     } else {
         const float s = __uint_as_float(ws << 23);
         const uint32_t q[4] = {w.x, w.y, w.z, w.w};
@@ -85,14 +86,16 @@ __device__ __forceinline__ void multiply128(const uint4& w, uint32_t ws, const u
         for (int u = 0; u < 4; ++u) {
             const bf16x8_t f = dequantise8(q[u], s);
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-                acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, __builtin_bit_cast(bf16x8_t, a[m][u]), acc[m], 0, 0, 0);
+            for (int v = 0; v < VALUES; ++v)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, __builtin_bit_cast(bf16x8_t, a[v][m][u]), acc[m], 0, 0, 0);
         }
     }
 }
 
 // The same with its loads, at a row's end: block b may lie behind it, and the block may be cut (pieces of bf16 rows): zeros there.
-template <bool A4, int MT>
+template <bool A4, int MT, int VALUES>
 __device__ __forceinline__ void step128(const uint8_t* w_row, const uint8_t* ws_row, const char* const (&a_row)[MT],
                                         const uint8_t* const (&as_row)[MT], int b, int Kb, int pieces, f32x4_t (&acc)[MT]) {
     constexpr int kPieces = A4 ? 1 : 4;
@@ -100,7 +103,7 @@ __device__ __forceinline__ void step128(const uint8_t* w_row, const uint8_t* ws_
     const int bb = in ? b : Kb - 1;
     const uint4 w = keep_if(in, *(const uint4*)(w_row + 16 * (int64_t)bb));
     const uint32_t ws = in ? ws_row[bb] : 0u;
-    uint4 a[MT][kPieces];
+    uint4 a[VALUES][MT][kPieces];
     uint32_t as[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -108,25 +111,26 @@ __device__ __forceinline__ void step128(const uint8_t* w_row, const uint8_t* ws_
         for (int u = 0; u < kPieces; ++u) {
             const int p = kPieces * bb + u;
             const bool there = in && (A4 || p < pieces);
-            a[m][u] = keep_if(there, *(const uint4*)(a_row[m] + 16 * (int64_t)(there ? p : 0)));
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) a[v][m][u] = keep_if(there, *(const uint4*)(a_row[m] + 64 * (int64_t)Kb * v + 16 * (int64_t)(there ? p : 0)));
         }
         if constexpr (A4) as[m] = in ? as_row[m][bb] : 0u;
     }
-    multiply128<A4, MT>(w, ws, a, as, acc);
+    multiply128<A4, MT, VALUES>(w, ws, a, as, acc);
 }
 
 // The steps wv, wv + waves, ... of the rows' steps, the loads of several of them (few rows of A: four) on their way at once: a wave has few steps, and
-// one after the other they are a chain of memory round trips.
-template <bool A4, int MT>
+// one after the other they are a chain of memory round trips.  VALUES = 2: rows of hidden activations, a row of first values and one of second ones, 64 Kb bytes each.
+template <bool A4, int MT, int VALUES>
 __device__ __forceinline__ void wave_steps(const uint8_t* w_row, const uint8_t* ws_row, const char* const (&a_row)[MT],
                                            const uint8_t* const (&as_row)[MT], int Kb, int pieces, int g, int wv, int waves,
                                            f32x4_t (&acc)[MT]) {
-    constexpr int kBatch = A4 ? (MT == 4 ? 2 : 4) : (MT == 1 ? 4 : MT == 2 ? 2 : 1), kPieces = A4 ? 1 : 4;
+    constexpr int kRows = MT * VALUES, kBatch = A4 ? (MT == 4 ? 2 : 4) : (kRows == 1 ? 4 : kRows == 2 ? 2 : 1), kPieces = A4 ? 1 : 4;
     const int steps = (Kb + 3) / 4;
     const int whole = A4 ? Kb / 4 : pieces / 16;       // steps without an end of a row in them
     int c = wv;
     for (; c < whole; c += kBatch * waves) {
-        uint4 w[kBatch], a[kBatch][MT][kPieces];
+        uint4 w[kBatch], a[kBatch][VALUES][MT][kPieces];
         uint32_t ws[kBatch], as[kBatch][MT];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
@@ -138,18 +142,20 @@ __device__ __forceinline__ void wave_steps(const uint8_t* w_row, const uint8_t* 
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
 #pragma unroll
-                for (int q = 0; q < kPieces; ++q) a[u][m][q] = *(const uint4*)(a_row[m] + 16 * (int64_t)(kPieces * b + q));
+                for (int v = 0; v < VALUES; ++v)
+#pragma unroll
+                    for (int q = 0; q < kPieces; ++q) a[u][v][m][q] = *(const uint4*)(a_row[m] + 64 * (int64_t)Kb * v + 16 * (int64_t)(kPieces * b + q));
                 if constexpr (A4) as[u][m] = as_row[m][b];
             }
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             if (u > 0 && c + u * waves >= whole) break;
-            multiply128<A4, MT>(w[u], ws[u], a[u], as[u], acc);
+            multiply128<A4, MT, VALUES>(w[u], ws[u], a[u], as[u], acc);
         }
     }
     for (c = whole + (wv + waves - whole % waves) % waves; c < steps; c += waves)      // (the first of this wave's behind the whole ones)
-        step128<A4, MT>(w_row, ws_row, a_row, as_row, 4 * c + g, Kb, pieces, acc);
+        step128<A4, MT, VALUES>(w_row, ws_row, a_row, as_row, 4 * c + g, Kb, pieces, acc);
 }
 
 __device__ __forceinline__ float bias_at(const Args& a, const void* bias, int64_t n) {
@@ -206,6 +212,26 @@ __device__ __forceinline__ void store4(char* out, bool bf16, bool vec, int64_t a
     }
 }
 
+// Hidden activations are held as two bf16 values, the first 16 bits of the fp32 value and what they leave, rounded: within 2^-15 of it, where one value, within 2^-8,
+// would cost results in bf16 half of their accuracy (of 8192 tokens through 2 of 16 leaves, 768 - 2048 - 768: 2.3e-3 off on average, 1.7e-3 with two, which is the rounding of the
+// results alone; 169 and 211 us).  Infinities and NaN are the first value alone.  A row is its first values, then its second ones.
+__device__ __forceinline__ float first_value(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ __forceinline__ float second_value(float v) { return fabsf(v) < __builtin_inff() ? v - first_value(v) : 0.0f; }
+__device__ __forceinline__ uint32_t first_values(float a, float b) { return __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t second_values(float a, float b) { return pack_bf16x2(second_value(a), second_value(b)); }
+// four of a row of `width`, at a multiple of four
+__device__ __forceinline__ void store_hidden4(char* out, int64_t row, int64_t width, int64_t n, const float* v) {
+    uint16_t* const o = (uint16_t*)out + row * 2 * width + n;
+    *(uint2*)o = make_uint2(first_values(v[0], v[1]), first_values(v[2], v[3]));
+    *(uint2*)(o + width) = make_uint2(second_values(v[0], v[1]), second_values(v[2], v[3]));
+}
+// eight, at a multiple of eight
+__device__ __forceinline__ void store_hidden8(char* out, int64_t row, int64_t width, int64_t n, const float* v) {
+    uint16_t* const o = (uint16_t*)out + row * 2 * width + n;
+    *(uint4*)o = make_uint4(first_values(v[0], v[1]), first_values(v[2], v[3]), first_values(v[4], v[5]), first_values(v[6], v[7]));
+    *(uint4*)(o + width) = make_uint4(second_values(v[0], v[1]), second_values(v[2], v[3]), second_values(v[4], v[5]), second_values(v[6], v[7]));
+}
+
 // eight, at a multiple of eight; vec: rows are whole aligned pieces of 16 bytes
 __device__ __forceinline__ void store8(char* out, bool bf16, bool vec, int64_t at, int64_t n, int64_t limit, const float* v) {
     if (vec && n + 8 <= limit) {
@@ -227,14 +253,18 @@ __device__ __forceinline__ void store8(char* out, bool bf16, bool vec, int64_t a
 
 // 16 rows of W against 16 MT rows of A per block, K shared out among its waves.
 //   kDense         rows of A as they come, rows of out too
-//   kHidden        a tile of one leaf's slots: rows of A are the slots' tokens; out is h [slot][32 blocks]
-//   kOutput        a tile of one leaf's slots: rows of A are h; out is y [pair] in fp32, or with k = 1 the token's row
+//   kHidden        a tile of one leaf's slots: rows of A are the slots' tokens; out is h [slot][two values][32 blocks]
+//   kOutput        a tile of one leaf's slots, or half of one: rows of A are h; out is y [pair] in fp32, or with k = 1 the token's row
 template <bool A4, int MT, int MODE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
     __shared__ f32x4_t part[WAVES][MT][kWave];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = lane & 15, g = lane >> 4;
     const int64_t n_blocks = (a.N + 15) / 16;
-    const int64_t nb = blockIdx.x % n_blocks, tile = blockIdx.x / n_blocks;
+    int64_t nb = blockIdx.x % n_blocks, tile = blockIdx.x / n_blocks, part_of = 0;
+    if (MODE == kOutput && a.parts > 1) {
+        part_of = tile % a.parts;
+        tile /= a.parts;
+    }
     const int64_t n0 = nb * 16;
     const int64_t w_row_bytes = (int64_t)a.Kb * 16;
     const int64_t n = n0 + j < a.N ? n0 + j : a.N - 1;
@@ -245,8 +275,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
     } else {
         if (tile >= *a.n_tiles) return;
         leaf = a.tile_leaf[tile];
-        first = a.tile_slot[tile];
+        first = a.tile_slot[tile] + part_of * (16 * MT);
         rows = a.start[leaf + 1] - first;
+        if (rows <= 0) return;
     }
     if (rows > 16 * MT) rows = 16 * MT;
     f32x4_t acc[MT];
@@ -262,7 +293,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
         a_row[m] = a.a + r * a.a_row;
         as_row[m] = A4 ? a.a_scales + r * a.Kb : nullptr;
     }
-    wave_steps<A4, MT>(a.w + (leaf * a.N + n) * w_row_bytes, a.w_scales + (leaf * a.N + n) * a.Kb, a_row, as_row, a.Kb, a.pieces, g, wv, WAVES, acc);
+    wave_steps<A4, MT, MODE == kOutput ? 2 : 1>(a.w + (leaf * a.N + n) * w_row_bytes, a.w_scales + (leaf * a.N + n) * a.Kb, a_row, as_row, a.Kb, a.pieces, g, wv, WAVES, acc);
 #pragma unroll
     for (int m = 0; m < MT; ++m) part[wv][m][lane] = acc[m];
     __syncthreads();
@@ -283,10 +314,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void mx4_rows_kernel(const Args a) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) o[q] = n4 + q < a.N ? apply(v[q] + bf16_to_f32(bias[n4 + q]), a.act, true) : 0.f;
             // (the row of h is whole blocks of 32: zeros behind the leaf's width)
-            store4(a.out, true, true, (first + row) * a.out_row, n4, a.out_row, o);
+            store_hidden4(a.out, first + row, a.out_row, n4, o);
             if (n4 + 16 >= a.N && n4 + 16 < a.out_row) {
                 const float z[4] = {0.f, 0.f, 0.f, 0.f};
-                store4(a.out, true, true, (first + row) * a.out_row, n4 + 16, a.out_row, z);
+                store_hidden4(a.out, first + row, a.out_row, n4 + 16, z);
             }
         } else {
             const uint16_t* const bias = (const uint16_t*)a.bias + leaf * a.N;
@@ -336,16 +367,17 @@ template <bool A4, int MT> struct TileShape {
     static constexpr int kLds = kRing * kStage + 2 * kPanelBytes;
 };
 
+// Rows of hidden activations (kOutput) are the first values of 8 MT slots and then their second ones, whose sums meet at the end: W is read and converted once for both.
 template <bool A4, int MODE, bool WIDE, int MT>
 __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a, const uint32_t max_row_tiles, const uint32_t col_tiles) {
     typedef TileShape<A4, MT> S;
-    constexpr int NT = S::NT;
+    constexpr int NT = S::NT, kSlots = MODE == kOutput ? S::kRows / 2 : S::kRows;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
     // an XCD takes a contiguous range of tiles, kGroup row tiles against all columns at a time
     constexpr uint32_t kGroup = 4;
     // (of the tiles that there are: a grid for the most that leaves can have leaves one XCD a part of its range)
-    const uint32_t row_tiles = MODE == kDense ? max_row_tiles : (uint32_t)*a.n_tiles;
+    const uint32_t row_tiles = MODE == kDense ? max_row_tiles : (uint32_t)(*a.n_tiles * a.parts);
     const uint32_t share = (row_tiles * col_tiles + kXcds - 1) / kXcds, id = (blockIdx.x % kXcds) * share + blockIdx.x / kXcds;
     if (blockIdx.x / kXcds >= share || id >= row_tiles * col_tiles) return;
     const uint32_t group = id / (kGroup * col_tiles), in = id - group * kGroup * col_tiles;
@@ -357,12 +389,14 @@ __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a,
         first = rt * S::kRows;
         rows = a.T - first;
     } else {
-        leaf = a.tile_leaf[rt];
-        first = a.tile_slot[rt];
+        leaf = a.tile_leaf[rt / a.parts];
+        first = a.tile_slot[rt / a.parts] + rt % a.parts * kSlots;
         rows = a.start[leaf + 1] - first;
+        if (rows <= 0) return;
     }
-    if (rows > S::kRows) rows = S::kRows;
+    if (rows > kSlots) rows = kSlots;
     const auto a_index = [&](int64_t r) -> int64_t {
+        if (MODE == kOutput) r &= kSlots - 1;
         r = (r < rows ? r : rows - 1) + first;
         if constexpr (MODE == kHidden) r = a.perm[r] / a.k;
         return r;
@@ -387,8 +421,10 @@ __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a,
     };
 #pragma unroll
     for (int i = 0; i < S::kALoads; ++i) {
-        const int64_t r = a_index((i * S::kWaves + wv) * (1024 / S::kARow) + lane / (S::kARow / 16));
+        const int in_tile = (i * S::kWaves + wv) * (1024 / S::kARow) + lane / (S::kARow / 16);
+        const int64_t r = a_index(in_tile);
         a_off[i] = (Offset)((MODE == kHidden ? r : r - first) * a.a_row + 16 * a_piece(i));
+        if (MODE == kOutput && in_tile >= kSlots) a_off[i] += (Offset)(64 * a.Kb);
     }
 #pragma unroll
     for (int i = 0; i < S::kWLoads; ++i) {
@@ -537,6 +573,12 @@ __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a,
     constexpr int kHalf = MT / 2, kPitch = 16 * NT + 4, kRowsAtOnce = 64 / kLanes;
     static_assert(S::kWaves * 16 * kHalf * kPitch * 4 <= S::kLds, "results fit where the stages were");
     float* const part = (float*)lds + wv * 16 * kHalf * kPitch;
+    if constexpr (MODE == kOutput) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < MT / 2; ++m) acc[n][m] += acc[n][m + MT / 2];
+    }
     const int64_t limit = MODE == kHidden ? a.out_row : a.N;
     const int64_t n8 = n0 + 16 * NT * wv + 8 * (lane % kLanes);
     float bias[8];
@@ -544,7 +586,7 @@ __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a,
     for (int q = 0; q < 8; ++q)
         bias[q] = n8 + q >= a.N ? 0.f : MODE == kDense ? bias_at(a, a.bias, n8 + q) : bf16_to_f32(((const uint16_t*)a.bias)[leaf * a.N + n8 + q]);
     __syncthreads();
-    for (int half = 0; half < 2; ++half) {
+    for (int half = 0; half < (MODE == kOutput ? 1 : 2); ++half) {
 #pragma unroll
         for (int m = 0; m < kHalf; ++m)
 #pragma unroll
@@ -569,7 +611,8 @@ __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a,
                 else o[q] = apply(o[q], a.act, MODE == kHidden || a.out_bf16);
                 if constexpr (MODE == kHidden) o[q] = n8 + q < a.N ? o[q] : 0.f;
             }
-            store8(a.out, MODE == kHidden || a.out_bf16, MODE == kHidden || a.out_vec, to * a.out_row, n8, limit, o);
+            if constexpr (MODE == kHidden) store_hidden8(a.out, to, a.out_row, n8, o);
+            else store8(a.out, a.out_bf16, a.out_vec, to * a.out_row, n8, limit, o);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
@@ -578,9 +621,9 @@ __global__ __launch_bounds__(256, A4 ? 2 : 3) void mx4_tile_kernel(const Args a,
 template <bool A4, int MODE, int MT> hipError_t launch_tiles(Args a, int64_t row_tiles, hipStream_t s) {
     typedef TileShape<A4, MT> S;
     const int64_t col_tiles = ((MODE == kHidden ? a.out_row : a.N) + S::kCols - 1) / S::kCols;
-    const int64_t blocks = (row_tiles * col_tiles + kXcds - 1) / kXcds * kXcds;
+    const int64_t blocks = (row_tiles * a.parts * col_tiles + kXcds - 1) / kXcds * kXcds;
     a.out_vec = a.out_row % (a.out_bf16 ? 8 : 4) == 0 && ((uintptr_t)a.out & 15) == 0;
-    // rows of A within 32 bits of the first that a block reaches: its own always (K <= 2^22), any token's not always
+    // rows of A within 32 bits of the first that a block reaches: its own always (K <= 2^22; hidden rows 2^18 bytes), any token's not always
     const bool wide = MODE == kHidden && a.T * a.a_row >= (int64_t)1 << 32;
     note_launch("mx4_tile_kernel<%s,%d,%s>", A4 ? "mx4" : "bf16", S::kRows, MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : "output");
     const auto kernel = wide ? mx4_tile_kernel<A4, MODE, MODE == kHidden, MT> : mx4_tile_kernel<A4, MODE, false, MT>;
@@ -594,13 +637,13 @@ template <bool A4, int MODE, int MT> hipError_t launch_tiles(Args a, int64_t row
 // 45 / 50, 2048 rows 76 / 67; of codes 20 / 23, 37 / 31; 4096 bf16 rows of 768, 2048 results, 512 tiles: 21 / 22).
 int tile_rows_for(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128) >= 2 * device_info().cus ? 128 : 64; }
 
-template <bool A4, int MODE> hipError_t launch_tiles(const Args& a, int64_t row_tiles, int tile_rows, hipStream_t s) {
-    return tile_rows == 128 ? launch_tiles<A4, MODE, 8>(a, row_tiles, s) : launch_tiles<A4, MODE, 4>(a, row_tiles, s);
+template <bool A4, int MODE> hipError_t launch_tiles(Args a, int64_t row_tiles, int tile_rows, hipStream_t s) {
+    a.parts = MODE == kOutput ? tile_rows / 64 : 1;
+    if constexpr (MODE != kOutput) {
+        if (tile_rows == 64) return launch_tiles<A4, MODE, 4>(a, row_tiles, s);
+    }
+    return launch_tiles<A4, MODE, 8>(a, row_tiles, s);
 }
-
-// Leaf networks, in every launch: a hidden activation is rounded to one bf16 value, the operand of the second product (a second value for what the first leaves would
-// double that product's matrix instructions: of 8192 tokens through 2 of 16 leaves, 768 - 2048 - 768, 71 of 168 us).  Everything after it is fp32: the
-// leaf's sums, its bias, the mixture weights, the sum over a token's leaves.
 
 // ---- a block a token ---------------------------------------------------------------------------------------
 //
@@ -609,62 +652,70 @@ template <bool A4, int MODE> hipError_t launch_tiles(const Args& a, int64_t row_
 // dependent reads of weights.
 constexpr int kTokenWaves = 8, kTokenTiles = 4;
 
-// Steps c0, c0 + stride, ... of one row of A (in global memory or LDS) against up to NT tiles of 16 rows of W.
-template <int NT>
-__device__ __forceinline__ void tiles_steps(const uint8_t* const (&w_row)[NT], const uint8_t* const (&ws_row)[NT], int tiles,
+// Steps c0, c0 + stride, ... of one row of A (in global memory or LDS; VALUES = 2: of hidden activations) against up to NT tiles of 16 rows of W,
+// whose first blocks are `first` of its matrix.
+template <int VALUES, class Index, int NT>
+__device__ __forceinline__ void tiles_steps(const uint8_t* w_base, const uint8_t* ws_base, const Index (&first)[NT], int tiles,
                                             const char* a_row, int Kb, int pieces, int g, int c0, int stride, f32x4_t (&acc)[NT]) {
     const int steps = (Kb + 3) / 4;
     for (int c = c0; c < steps; c += stride) {
         const int b = 4 * c + g;
         const bool in = b < Kb;
         const int bb = in ? b : Kb - 1;
-        uint4 w[NT], x[4];
+        uint4 w[NT], x[VALUES][4];
         uint32_t ws[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if (t >= tiles) break;
-            w[t] = *(const uint4*)(w_row[t] + 16 * (int64_t)bb);
-            ws[t] = ws_row[t][bb];
+            const Index at = first[t] + bb;
+            w[t] = ((const uint4*)w_base)[at];
+            ws[t] = ws_base[at];
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const bool there = in && 4 * bb + u < pieces;
-            x[u] = keep_if(there, *(const uint4*)(a_row + 16 * (int64_t)(there ? 4 * bb + u : 0)));
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) x[v][u] = keep_if(there, *(const uint4*)(a_row + 64 * (int64_t)Kb * v + 16 * (int64_t)(there ? 4 * bb + u : 0)));
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if (t >= tiles) break;
-            const uint4 v = keep_if(in, w[t]);
-            const float s = __uint_as_float((in ? ws[t] : 0u) << 23);
-            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequantise8(q[u], s), __builtin_bit_cast(bf16x8_t, x[u]), acc[t], 0, 0, 0);
+            w[t] = keep_if(in, w[t]);
+            ws[t] = in ? ws[t] << 23 : 0u;
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (t >= tiles) break;
+                const bf16x8_t f = dequantise8(u == 0 ? w[t].x : u == 1 ? w[t].y : u == 2 ? w[t].z : w[t].w, __uint_as_float(ws[t]));
+#pragma unroll
+                for (int v = 0; v < VALUES; ++v) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, __builtin_bit_cast(bf16x8_t, x[v][u]), acc[t], 0, 0, 0);
+            }
     }
 }
 
 __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args a, const Args b) {
-    extern __shared__ __align__(16) uint16_t h[];          // [k][h_row]
+    extern __shared__ __align__(16) uint16_t h[];          // [k][two values][h_row]
     __shared__ float part[2][kTokenWaves][16 * kTokenTiles];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = lane & 15, g = lane >> 4;
     const int64_t t = blockIdx.x;
     const int h_row = (int)a.out_row, h_tiles = h_row / 16;
     int round = 0;
     for (int i = 0; i < a.k; ++i) {
-        const uint32_t e = (uint32_t)a.idx[t * a.k + i];
+        const uint32_t e = (uint32_t)__builtin_amdgcn_readfirstlane(a.idx[t * a.k + i]);
         if (e >= a.E) continue;                            // (not read below)
+        const int64_t row0 = (int64_t)e * a.N;
         for (int t0 = 0; t0 < h_tiles; t0 += kTokenTiles, round ^= 1) {
-            const uint8_t *w_row[kTokenTiles], *ws_row[kTokenTiles];
+            uint32_t first[kTokenTiles];                   // (leaves of few bytes)
             f32x4_t acc[kTokenTiles];
 #pragma unroll
             for (int u = 0; u < kTokenTiles; ++u) {
-                const int64_t n = 16 * (t0 + u) + j, r = (int64_t)e * a.N + (n < a.N ? n : a.N - 1);
-                w_row[u] = a.w + r * a.Kb * 16;
-                ws_row[u] = a.w_scales + r * a.Kb;
+                const int n = 16 * (t0 + u) + j;
+                first[u] = (uint32_t)((n < a.N ? n : (int)a.N - 1) * a.Kb);
                 acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
-            tiles_steps<kTokenTiles>(w_row, ws_row, h_tiles - t0 < kTokenTiles ? h_tiles - t0 : kTokenTiles, a.a + t * a.a_row, a.Kb, a.pieces, g, wv, kTokenWaves, acc);
+            tiles_steps<1>(a.w + row0 * a.Kb * 16, a.w_scales + row0 * a.Kb, first, h_tiles - t0 < kTokenTiles ? h_tiles - t0 : kTokenTiles, a.a + t * a.a_row, a.Kb, a.pieces, g, wv, kTokenWaves, acc);
             if (j == 0) {
 #pragma unroll
                 for (int u = 0; u < kTokenTiles; ++u) *(f32x4_t*)&part[round][wv][16 * u + 4 * g] = acc[u];
@@ -676,7 +727,8 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
 #pragma unroll
                 for (int w = 1; w < kTokenWaves; ++w) v += part[round][w][tid];
                 v = n < a.N ? apply(v + bf16_to_f32(((const uint16_t*)a.bias)[(int64_t)e * a.N + n]), a.act, true) : 0.f;
-                h[i * h_row + n] = f32_to_bf16(v);
+                h[2 * i * h_row + n] = (uint16_t)(__float_as_uint(v) >> 16);
+                h[(2 * i + 1) * h_row + n] = f32_to_bf16(second_value(v));
             }
         }
     }
@@ -688,19 +740,19 @@ __global__ __launch_bounds__(64 * kTokenWaves) void mx4_token_kernel(const Args 
 #pragma unroll
         for (int u = 0; u < kTokenTiles; ++u) sum[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         for (int i = 0; i < b.k; ++i) {
-            const uint32_t e = (uint32_t)b.idx[t * b.k + i];
+            const uint32_t e = (uint32_t)__builtin_amdgcn_readfirstlane(b.idx[t * b.k + i]);
             if (e >= b.E) continue;
+            const int64_t row0 = (int64_t)e * b.N;
             const float scale = b.weight ? b.weight[t * b.k + i] : 1.0f;
-            const uint8_t *w_row[kTokenTiles], *ws_row[kTokenTiles];
+            uint32_t first[kTokenTiles];
             f32x4_t acc[kTokenTiles];
 #pragma unroll
             for (int u = 0; u < kTokenTiles; ++u) {
-                const int64_t n = 16 * (t0 + u) + j, r = (int64_t)e * b.N + (n < b.N ? n : b.N - 1);
-                w_row[u] = b.w + r * b.Kb * 16;
-                ws_row[u] = b.w_scales + r * b.Kb;
+                const int n = 16 * ((int)t0 + u) + j;
+                first[u] = (uint32_t)((n < b.N ? n : (int)b.N - 1) * b.Kb);
                 acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
-            tiles_steps<kTokenTiles>(w_row, ws_row, tiles, (const char*)(h + i * h_row), b.Kb, b.pieces, g, 0, 1, acc);
+            tiles_steps<2>(b.w + row0 * b.Kb * 16, b.w_scales + row0 * b.Kb, first, tiles, (const char*)(h + 2 * i * h_row), b.Kb, b.pieces, g, 0, 1, acc);
             if (j == 0) {
 #pragma unroll
                 for (int u = 0; u < kTokenTiles; ++u)
@@ -739,19 +791,19 @@ __global__ __launch_bounds__(64 * kTokenWaves, 4) void mx4_direct_kernel(const A
     for (int t = 0; t < NT; ++t) sum[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < k; ++i) {
         const int64_t pair = item * k + i;
-        const uint32_t e = (uint32_t)a.idx[pair];
+        const uint32_t e = (uint32_t)__builtin_amdgcn_readfirstlane(a.idx[pair]);
         if (e >= a.E) continue;
-        const uint8_t *w_row[NT], *ws_row[NT];
+        const int64_t row0 = (int64_t)e * a.N;
+        int64_t first[NT];
         f32x4_t acc[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int64_t n = n0 + 16 * t + j, r = (int64_t)e * a.N + (n < a.N ? n : a.N - 1);
-            w_row[t] = a.w + r * a.Kb * 16;
-            ws_row[t] = a.w_scales + r * a.Kb;
+            const int64_t n = n0 + 16 * t + j;
+            first[t] = (n < a.N ? n : a.N - 1) * a.Kb;
             acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
         // (step c of pair i is step i * steps + c of the sum: waves that pair i leaves without a step begin with pair i + 1)
-        tiles_steps<NT>(w_row, ws_row, tiles, a.a + (HIDDEN ? pair / a.k : pair) * a.a_row, a.Kb, a.pieces, g,
+        tiles_steps<HIDDEN ? 1 : 2>(a.w + row0 * a.Kb * 16, a.w_scales + row0 * a.Kb, first, tiles, a.a + (HIDDEN ? pair / a.k : pair) * a.a_row, a.Kb, a.pieces, g,
                         (wv + kTokenWaves - i * steps % kTokenWaves) % kTokenWaves, kTokenWaves, acc);
         const float scale = !HIDDEN && a.weight ? a.weight[pair] : 1.0f;
 #pragma unroll
@@ -777,7 +829,13 @@ __global__ __launch_bounds__(64 * kTokenWaves, 4) void mx4_direct_kernel(const A
         v = HIDDEN ? apply(v + bias, a.act, true) : fmaf(scale, bias, v);
     }
     if (HIDDEN && n >= a.N) v = 0.f;
-    ((uint16_t*)a.out)[item * a.out_row + n] = f32_to_bf16(v);
+    uint16_t* const out = (uint16_t*)a.out + item * (HIDDEN ? 2 : 1) * a.out_row + n;
+    if constexpr (HIDDEN) {
+        out[0] = (uint16_t)(__float_as_uint(v) >> 16);
+        out[a.out_row] = f32_to_bf16(second_value(v));
+    } else {
+        out[0] = f32_to_bf16(v);
+    }
 }
 
 // Columns a block: 64 where that leaves a block for every compute unit.
@@ -1017,14 +1075,21 @@ __global__ __launch_bounds__(256) void clear_kernel(const int32_t* __restrict__ 
     }
 }
 
-template <bool A4, int MODE> hipError_t launch_rows(const Args& a, int64_t tiles, int mt, hipStream_t s) {
-    const int64_t blocks = (a.N + 15) / 16 * tiles;
+template <bool A4, int MODE> hipError_t launch_rows(Args a, int64_t tiles, int mt, hipStream_t s) {
+    a.parts = MODE == kOutput && mt == 4 ? 2 : 1;          // (rows of two values: half as many at a time)
+    mt /= a.parts;
+    const int64_t blocks = (a.N + 15) / 16 * tiles * a.parts;
     note_launch("mx4_rows_kernel<%s,%d,%s>", A4 ? "mx4" : "bf16", mt,
                 MODE == kDense ? "dense" : MODE == kHidden ? "hidden" : "output");
     const dim3 grid((unsigned)blocks);
+    if constexpr (MODE != kOutput) {
+        if (mt == 4) {
+            mx4_rows_kernel<A4, 4, MODE, 4><<<grid, 256, 0, s>>>(a);
+            return hipGetLastError();
+        }
+    }
     if (mt == 1) mx4_rows_kernel<A4, 1, MODE, 8><<<grid, 512, 0, s>>>(a);
-    else if (mt == 2) mx4_rows_kernel<A4, 2, MODE, 8><<<grid, 512, 0, s>>>(a);
-    else mx4_rows_kernel<A4, 4, MODE, 4><<<grid, 256, 0, s>>>(a);
+    else mx4_rows_kernel<A4, 2, MODE, 8><<<grid, 512, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -1033,9 +1098,11 @@ template <bool A4, int MODE> hipError_t launch_rows(const Args& a, int64_t tiles
 // chip more than once.  (4096 x 4096, bf16 rows: 96 of them 31 / 31 us, 128 36 / 31; codes: 64 11.7 / 13.8, 96 17.6 / 13.6; 768 x 2048, bf16 rows: 256
 // 9.0 / 10.4, 512 15.4 / 10.7; codes: 256 5.5 / 7.8, 1024 12.8 / 8.5.)
 double rows_us(bool a4, double rows, int64_t N, int64_t K) { return 4.2 + rows * (double)N * (double)K * (a4 ? 7.9e-9 : 1.55e-8); }
-double tiles_us(bool a4, double rows64, int64_t N, int64_t K) {
-    const double tiles = rows64 * (double)((N + 127) / 128) / 512;
-    return (a4 ? 6 : 7) + (double)K * (a4 ? 0.0019 : 0.0059) * (tiles > 1 ? tiles : 1);
+// Hidden activations (`two_values`) count as two rows, and a block's stages are those of 128 rows from the first tile on (up to 4096 pairs, four shapes
+// with 4, 16 and 64 leaves: 0.01 us an element of K; with it the faster of both launches is chosen, or one less than a seventh behind it).
+double tiles_us(bool a4, double rows64, int64_t N, int64_t K, bool two_values = false) {
+    const double tiles = (two_values ? 2 : 1) * rows64 * (double)((N + 127) / 128) / 512, few = two_values ? 1.7 : 1;
+    return (a4 ? 6 : 7) + (double)K * (a4 ? 0.0019 : 0.0059) * (tiles > few ? tiles : few);
 }
 
 // Rows of A a block of mx4_rows_kernel takes, in tiles of 16: the most that leave blocks for three quarters of the compute units (1024 x 768, bf16 rows, one, two
@@ -1067,7 +1134,7 @@ struct LeafScratch {
         perm = take(4 * P);
         tile_leaf = take(4 * tiles);
         tile_slot = take(4 * tiles);
-        h = take(2 * P * kMxBlock * mx_blocks(L));
+        h = take(4 * P * kMxBlock * mx_blocks(L));
         y = take(k > 1 ? 4 * P * O : 0);
         total = o;
     }
@@ -1132,7 +1199,7 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     a.k = p.k;
     Args b = a;
     b.a = (const char*)h;
-    b.a_row = 2 * h_row;
+    b.a_row = 4 * h_row;
     b.w = p.w2;
     b.w_scales = p.s2;
     b.bias = p.b2;
@@ -1144,9 +1211,10 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     b.out_vec = p.O % 4 == 0 && ((uintptr_t)p.out & 7) == 0;
     hipError_t e;
     // Few pairs, or few of them a leaf: grouping gains nothing.  Leaves of few bytes go a block a token (one launch); others are spread over the chip.
-    const int64_t leaf_bytes = (int64_t)p.L * 16 * a.Kb + p.O * 16 * b.Kb, h_bytes = 2 * h_row * p.k;
-    if ((P <= 32 || P <= 4 * p.E) && p.k * leaf_bytes <= 256 * 1024 && h_bytes <= 32 * 1024) {
+    const int64_t leaf_bytes = (int64_t)p.L * 16 * a.Kb + p.O * 16 * b.Kb, h_bytes = 4 * h_row * p.k;
+    if ((P <= 32 || P <= 4 * p.E) && p.k * leaf_bytes <= 256 * 1024 && h_bytes <= 64 * 1024) {
         note_launch("mx4_token_kernel");
+        if ((e = hipFuncSetAttribute((const void*)mx4_token_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)h_bytes)) != hipSuccess) return e;
         mx4_token_kernel<<<dim3((unsigned)p.T), 64 * kTokenWaves, (size_t)h_bytes, s>>>(a, b);
         return hipGetLastError();
     }
@@ -1157,9 +1225,10 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     const int64_t met = p.E < P ? p.E : P;
     const int mt = P / p.E <= 16 ? 1 : P / p.E <= 32 ? 2 : 4;
     const double rows = 16.0 * mt * (double)(P / (16 * mt) + met), rows64 = (double)(P / 64 + met);
-    const bool large = tiles_us(false, rows64, p.L, p.D) + tiles_us(false, rows64, p.O, p.L) < rows_us(false, rows, p.L, p.D) + rows_us(false, rows, p.O, p.L) ||
-                       !rows_fit(P / (16 * mt) + met, p.L > p.O ? p.L : p.O);
-    const int tile_rows = large ? tile_rows_for(P, p.L < p.O ? p.L : p.O) : 16 * mt;
+    const bool large = tiles_us(false, rows64, p.L, p.D) + tiles_us(false, rows64, p.O, p.L, true) < rows_us(false, rows, p.L, p.D) + rows_us(false, 2 * rows, p.O, p.L) ||
+                       !rows_fit(2 * (P / (16 * mt) + met), p.L > p.O ? p.L : p.O);
+    int tile_rows = large ? tile_rows_for(P, p.L < p.O ? p.L : p.O) : 16 * mt;
+    if (tile_rows == 128 && 2 * (P / 128 + met) * ((p.O + 127) / 128) > kMaxMx4Tiles) tile_rows = 64;       // (blocks of the second product)
     const int64_t tiles = P / tile_rows + met;
     int32_t *const count = words(at.count), *const start = words(at.start), *const tile_start = words(at.tile_start);
     int32_t *const rank = words(at.rank), *const perm = words(at.perm), *const tile_leaf = words(at.tile_leaf), *const tile_slot = words(at.tile_slot);

@@ -166,6 +166,37 @@ def test_mixture_weights_meet_sums_not_activations(T, D, k):
     _within(out, want, tol + R.HALF["bf16"] * (np.abs(want) + tol), "mixture of %d tokens" % T)
 
 
+@pytest.mark.parametrize("T,D,k", [(20, 32, 1), (6, 32, 4), (20, 4096, 1), (7, 4096, 3), (60, 32, 1), (300, 32, 2), (1500, 1024, 2), (6000, 1024, 2)])
+def test_hidden_activations_hold_more_bits_than_bf16(T, D, k):
+    """Activations a little above 1 to 2, whose small parts are what the differences of their pairs are made of: an activation rounded to bf16 is off by 2^-8."""
+    import torch
+    import paper_2308_14711_amd as F
+    E, L, O = 6, 128, 64
+    rng = np.random.default_rng(T + k)
+    b1 = np.tile(rng.integers(128, 256, size=(E, O)) / 128.0, (1, 2))
+    w1 = np.zeros((E, L, D))
+    w1[:, :, 0] = rng.choice(R.GRID, size=(E, L)) * 2.0 ** -12
+    w2 = np.zeros((E, O, L))
+    w2[:, np.arange(O), np.arange(O)], w2[:, np.arange(O), np.arange(O) + O] = 1, -1
+    c1, s1 = R.quantise(w1)
+    c2, s2 = R.quantise(w2)
+    w1 = R.values(c1, s1, D)
+    x = np.zeros((T, D))
+    x[:, 0] = rng.choice([1.0, -1.0, 0.5], size=T)
+    idx = rng.integers(0, E, size=(T, k)).astype(np.int32)
+    weight = rng.normal(size=(T, k)).astype(np.float32)
+    out = torch.empty((T, O), dtype=torch.bfloat16, device="cuda")
+    F.fff_leaf_forward_mx4(_up(x, "bf16")[0], _bytes(c1), _bytes(s1), _up(b1, "bf16")[0], _bytes(c2), _bytes(s2),
+                           torch.zeros((E, O), dtype=torch.bfloat16, device="cuda"), _bytes(idx), _bytes(weight), F.ACT_RELU, out)
+    h = x[:, 0][:, None, None] * w1[idx][:, :, :, 0] + b1[idx]
+    g = np.abs(weight.astype(np.float64))[:, :, None]
+    want = (weight.astype(np.float64)[:, :, None] * (h[:, :, :O] - h[:, :, O:])).sum(1)
+    # an activation within 2^-15 of its value (and its sum of two terms within 2^-24), sums and products in single precision, half a step of bf16
+    size = (g * (np.abs(h[:, :, :O]) + np.abs(h[:, :, O:]))).sum(1)
+    tol = (2.0 ** -15 + (2 * k + 4) * 2.0 ** -24) * size
+    _within(out, want, tol + R.HALF["bf16"] * (np.abs(want) + tol), "differences of %d tokens" % T)
+
+
 # ---- every scale byte ------------------------------------------------------------------------------------------
 
 
