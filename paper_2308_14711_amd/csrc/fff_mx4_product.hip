@@ -1214,7 +1214,7 @@ hipError_t launch_mx4_leaves(const Mx4Leaves& p, void* scratch, hipStream_t s) {
     const int64_t leaf_bytes = (int64_t)p.L * 16 * a.Kb + p.O * 16 * b.Kb, h_bytes = 4 * h_row * p.k;
     if ((P <= 32 || P <= 4 * p.E) && p.k * leaf_bytes <= 256 * 1024 && h_bytes <= 64 * 1024) {
         note_launch("mx4_token_kernel");
-        if ((e = hipFuncSetAttribute((const void*)mx4_token_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)h_bytes)) != hipSuccess) return e;
+        if (h_bytes > 56 * 1024 && (e = hipFuncSetAttribute((const void*)mx4_token_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)h_bytes)) != hipSuccess) return e;
         mx4_token_kernel<<<dim3((unsigned)p.T), 64 * kTokenWaves, (size_t)h_bytes, s>>>(a, b);
         return hipGetLastError();
     }

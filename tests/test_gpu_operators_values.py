@@ -308,3 +308,16 @@ def test_many_tokens_of_few_leaves(E, T, k):
     # k products and sums in single precision, half a step of bf16
     tol = 2 * k * 2.0 ** -24 * size
     _within(out, want, tol + R.HALF["bf16"] * (np.abs(want) + tol), "biases")
+
+
+def test_a_token_s_activations_that_fill_a_block_s_lds():
+    """32 leaves a token, 470 neurons of two values each: 60 KB, in one launch."""
+    import torch
+    import paper_2308_14711_amd as F
+    rng = np.random.default_rng(60)
+    dev, ref = _leaf_case(rng, 3, 32, 40, 20, 1, 470, True)
+    out = torch.full((3, 1), -7.0, dtype=torch.bfloat16, device="cuda")
+    F.fff_leaf_forward_mx4(*dev, F.ACT_GELU, out)
+    assert F.fff_last_launch().endswith("mx4_token_kernel"), F.fff_last_launch()
+    want, tol = R.leaves(*ref, "gelu")
+    _within(out, want, tol, "leaves")
