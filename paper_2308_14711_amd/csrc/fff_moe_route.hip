@@ -7,8 +7,8 @@
 // and leaves as one row per block; a second launch adds the rows of the blocks up, always in the same order.
 // The gradient is one pass as well: with c[e] = dloss[0] E f[e] / n, p and lse from the logits again,
 //   dlogits[e] = p[e] (c[e] - sum_j c[j] p[j] + 2 dloss[1] lse / n) + the weights' part on the k chosen.
-// The gradient is bound by the bytes of the logits and their gradient (32768 x 512 in fp32, 134 MB: 32 us, 4.1 TB/s), the forward pass by vector
-// work and LDS round trips (8 chosen there: 29 us, where bytes alone would take 13).
+// The gradient is near the time of the bytes of the logits and their gradient (32768 x 512 in fp32, 134 MB: 34 us, 4.0 TB/s), the forward pass is vector
+// work and waits for lanes and LDS (8 chosen there: 34 us, where bytes alone would take 13; vector units busy 54 % of the cycles).
 #include "fff_device.h"
 #include "fff_mx4.h"
 
