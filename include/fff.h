@@ -303,7 +303,8 @@ size_t fff_mx4_product_scratch_bytes(int64_t T, int64_t K);
  *   leaf_w2, leaf_s2: codes and scales of [n_leaves, O, leaf_width] (of leaf_w2 [n_leaves, leaf_width, O]:
  *   fff_mx4_quantize with transpose); leaf_b2 [n_leaves, O]; biases bf16
  *   (the matrices' values as bf16 has them: fff_mx4_product)
- *   leaf_idx [T, k] int32, weight [T, k] fp32 or NULL (ones); k 1..32; n_leaves 1..65536; leaf_width 1..65536
+ *   leaf_idx [T, k] int32, weight [T, k] fp32 or NULL (ones; an infinite one may make its token NaN, since it meets parts of
+ *   a leaf's sum); k 1..32; n_leaves 1..65536; leaf_width 1..65536
  *   act FFF_ACT_RELU or FFF_ACT_GELU; out [T, O] bf16, must not overlap x; dtype must be FFF_BF16 (else FFF_ERR_UNSUPPORTED)
  *   scratch  device memory, 256-byte aligned, of one call until its launches have run, at least
  *            fff_leaf_mx4_scratch_bytes of the same sizes; needs no initial value
